@@ -11,8 +11,9 @@
  *   - n_i = kept tokens of image i, T = sum_i n_i = cu_seqlens[B].
  *   - Every pointer except `stream` is a DEVICE pointer owned by the caller.  The library never
  *     allocates, frees or keeps a pointer, never synchronises and never copies to the host: each
- *     call enqueues exactly one kernel on `stream` and returns, so all calls are legal inside a
- *     HIP stream capture.  T is never read on the host; grids are sized by upper bounds and
+ *     call enqueues exactly one kernel on `stream` (ragged_layernorm_backward and ragged_grad_clip:
+ *     two) and returns, so all calls are legal inside a HIP stream capture.  The two calls that only
+ *     prepare host data (ragged_rope_frequencies, ragged_grad_plan) enqueue nothing and take HOST pointers.  T is never read on the host; grids are sized by upper bounds and
  *     surplus work-groups exit on the device.
  *   - `stream` is a hipStream_t passed as void*; NULL is the default stream.
  *   - 16-bit floating rows are moved as raw words by pack / unpack (bit copy).
@@ -295,6 +296,124 @@ int ragged_layernorm(const void* x, const void* gamma, const void* beta, void* y
  */
 int ragged_token_scores_l2(const void* x, int64_t rows, int C, ragged_dtype dt, double* scores, void* stream);
 int ragged_keep_topk(const double* scores, int B, int N, int k, uint8_t* keep, void* stream);
+
+/*
+ * ---- Training on packed rows ---------------------------------------------------------------------
+ * What the encoder blocks of Section 4.3 (item 4) need on the way back, on the same packed rows: positions that survive packing,
+ * attention with its gradients, LayerNorm's gradients, and the norm and clipping of a model's gradients.  Rows beyond the valid ones are
+ * neither read nor written, as everywhere here.
+ *
+ * ragged_rope -- rotary positions: in every head the first 2 * pairs elements are rotated, two by two,
+ *     y[a] = m (x[a] cos t - x[b] sin t),   y[b] = m (x[a] sin t + x[b] cos t),   t = coords[c, axis(p)] * freqs[p]
+ * for pair p = 0 .. pairs - 1; the other elements of the head are passed on.  One launch for query and key rows.
+ *
+ *   q, q_out   [rows, Hq, D]  rows q_stride / q_out_stride elements apart, [Hq, D] contiguous inside a row (dt)
+ *   k, k_out   [rows, Hk, D]  the same with k_stride / k_out_stride and their own number of heads; both NULL: no keys
+ *              q_out may be q (then with the same stride) and k_out may be k; other overlaps are not allowed
+ *   rows_cap, rows_dev        as for ragged_linear
+ *   coords     [n_coords, axes]  fp32 positions; row r has those of line  u mod n_coords,  u = index[r] as an unsigned number
+ *                             (index NULL: r itself).  Packed rows of images pass gather_idx and the N tokens' coordinates, text passes
+ *                             its positions and the numbers 0 .. n_coords - 1
+ *   freqs      [pairs]        fp64 radians per unit (see ragged_rope_frequencies); axis(p) = p / (pairs / axes): with two
+ *                             axes the first half of the pairs turns with coords[., 0], the second with coords[., 1]
+ *   layout     0: half, a = p, b = pairs + p;  1: interleaved, a = 2 p, b = 2 p + 1
+ *   amplitude  m; inverse 1: t negated.  The rotation's transpose, which takes gradients back, is inverse 1 with the same m
+ *
+ * Angles are formed and brought to one turn in fp64, sines, cosines and the rotation are fp32, one rounding to dt.
+ * Supported: dt = F16 or BF16, D a multiple of 8 and <= 512, 1 <= pairs <= D / 2, pairs a multiple of axes, (Hq + Hk) * D <= 2^22,
+ * strides multiples of 8 that hold a row and < 2^31, finite amplitude.
+ */
+int ragged_rope(const void* q, const void* k, void* q_out, void* k_out, int64_t rows_cap, const int32_t* rows_dev, int Hq, int Hk, int D,
+                int64_t q_stride, int64_t k_stride, int64_t q_out_stride, int64_t k_out_stride, const float* coords, int64_t n_coords,
+                int axes, const int32_t* index, const double* freqs, int pairs, int layout, float amplitude, int inverse,
+                ragged_dtype dt, void* stream);
+
+/*
+ * ragged_rope_frequencies -- the frequencies of one axis, P pairs, into HOST memory (an axis' part of freqs above):
+ *     f[p] = base^(-p / P)
+ *   scaling 0: as they are;  1: f / factor (positions interpolated);  2: with base * factor^(P / (P - 1)) for base: the highest
+ *   frequency stays, the lowest is divided by factor (P = 1: stays);  3: by parts: with r = original_length * f / (2 pi) turns over the
+ *   original length and g = (r - slow) / (fast - slow) held to [0, 1],  f * g + f / factor * (1 - g): what turns often stays, what turns
+ *   seldom is interpolated.
+ * base, factor > 0; scaling 3: original_length > 0, fast > slow.  The last three are not looked at otherwise.
+ */
+int ragged_rope_frequencies(double* freqs, int pairs, double base, int scaling, double factor, double original_length, double fast, double slow);
+
+/*
+ * ragged_attn_lse -- ragged_attn_strided that also writes what the backward pass needs of it:
+ *   lse        [T, H]   fp32 out: lse[s + r, h] = ln sum_j exp( scale * q[s+r, h, :] . k[s+j, h, :] ); rows >= T are left untouched
+ * o has the dtype of the inputs and is bit-identical to ragged_attn_strided's with the same arguments.
+ */
+int ragged_attn_lse(const void* q, const void* k, const void* v, void* o, float* lse, const int32_t* cu_seqlens, int B, int max_seqlen, int H,
+                    int D, int64_t in_tok_stride, int64_t out_tok_stride, float scale, ragged_dtype dt, void* stream);
+
+/*
+ * ragged_attn_backward -- the gradients of q, k and v of ragged_attn_lse, given that of o, in one launch:
+ *     P = exp(scale q k^T - lse),  dS = P * (dO v^T - rowsum(dO * o)),  dv = P^T dO,  dq = scale dS k,  dk = scale dS^T q
+ *
+ *   q, k, v    [T, H, D]  as given to ragged_attn_lse, in_tok_stride elements between tokens
+ *   o, d_o     [T, H, D]  its output and that output's gradient, out_tok_stride elements between tokens
+ *   lse        [T, H]     as it wrote them
+ *   dq, dk, dv [T, H, D]  out (dt), grad_tok_stride elements between tokens (for example the slices of a fused [T, 3, H, D] buffer);
+ *                         they must not overlap any input.  Rows >= T are left untouched
+ *   max_seqlen            an upper bound on every n_i; rows of sequences at positions >= 64 * ceil(max_seqlen / 64) are not computed,
+ *                         and their gradients are left untouched
+ *
+ * Supported: D = 64, dt = F16 or BF16; every token row on a 16-byte boundary; strides as for ragged_attn_strided (grad_tok_stride as
+ * out_tok_stride).  max_seqlen <= 64 * 32767 and half of the work-groups of ragged_attn's limit.  Products on MFMA with fp32 sums;
+ * P and dS are rounded to dt in between (with fp16, |dS| beyond 65504 overflows as the gradients themselves would).
+ * No atomics: results are bit-reproducible, and those of a sequence do not depend on the other sequences or on max_seqlen.
+ */
+int ragged_attn_backward(const void* q, const void* k, const void* v, const void* o, const void* d_o, const float* lse, void* dq, void* dk,
+                         void* dv, const int32_t* cu_seqlens, int B, int max_seqlen, int H, int D, int64_t in_tok_stride,
+                         int64_t out_tok_stride, int64_t grad_tok_stride, float scale, ragged_dtype dt, void* stream);
+
+/*
+ * ragged_layernorm_backward -- the gradients of ragged_layernorm.  With xh = (x - mean) / sqrt(var + eps) and w = gamma * dy, row by row:
+ *     dx = (w - mean(w) - xh mean(w xh)) / sqrt(var + eps)  [+ residual_grad],   dgamma = sum_rows dy xh,   dbeta = sum_rows dy
+ *
+ *   x, dy, dx      [rows_cap, C] (dt); gamma [C] (dt); dx may be dy or residual_grad (each element is read before it is written, by
+ *                  the same thread), and must not be x
+ *   residual_grad  [rows_cap, C] (dt) or NULL: the gradient that reaches x past the LayerNorm (x + f(LN(x)))
+ *   dgamma, dbeta  [C] fp32 out (0 where there are no rows)
+ *   workspace      ragged_layernorm_backward_workspace(rows_cap, C) bytes, 16-byte aligned; its contents before and after the call mean
+ *                  nothing, and calls that may run at the same time (other streams, other captured graphs) need one each
+ *   rows_dev       as for ragged_linear
+ * Nothing of the forward pass is needed but x.  Types and widths as for ragged_layernorm; two kernels; sums in one order (bit-reproducible).
+ */
+int64_t ragged_layernorm_backward_workspace(int64_t rows_cap, int C);      /* bytes; 0 for sizes that are not supported */
+int ragged_layernorm_backward(const void* x, const void* gamma, const void* dy, const void* residual_grad, void* dx, float* dgamma,
+                              float* dbeta, void* workspace, int64_t rows_cap, const int32_t* rows_dev, int C, float eps, ragged_dtype dt,
+                              void* stream);
+
+/*
+ * ragged_grad_plan and ragged_grad_clip -- the norm over the gradients of a whole model, and the gradients clipped by it:
+ *     norm = |scale| * sqrt( sum over all tensors of g^2 ),   dst = g * scale * min(1, max_norm / (norm + 1e-6))
+ * scale undoes a loss scale (1 otherwise).  A norm that is infinite or no number clips nothing (dst = g * scale): it is written all the
+ * same, and whoever steps the weights looks at it there.
+ *
+ * ragged_grad_plan lays the tensors out once, as a table of equal pieces in HOST memory, which the caller copies to the device:
+ *   tensors    [n]  host array: src and dst are DEVICE pointers (aligned to their own values), numel >= 0; src_dt F16, BF16 or F32, dst_dt
+ *                   the same or F32.  dst may be src (then of the same dtype) or NULL (the tensor counts for the norm only); other
+ *                   overlaps are not allowed
+ *   table      host memory of capacity bytes, or NULL to learn the size;  chunks: out, host: RAGGED_GRAD_CHUNK_BYTES of table each
+ * ragged_grad_clip runs it (two kernels):
+ *   table      the table in DEVICE memory, 16-byte aligned, chunks as given back
+ *   workspace  RAGGED_GRAD_WORKSPACE bytes, 16-byte aligned; calls that may run at the same time need one each
+ *   norm       [1] fp64 out, 8-byte aligned
+ *   max_norm   > 0, may be infinite (no clipping);  scale finite
+ * Squares and their sums are fp64, in one order (bit-reproducible).  With dst = src and a factor of 1 nothing is rewritten.
+ */
+#define RAGGED_GRAD_CHUNK_BYTES 32
+#define RAGGED_GRAD_WORKSPACE 16384
+typedef struct {
+    const void* src;
+    void* dst;
+    int64_t numel;
+    int32_t src_dt, dst_dt;      /* ragged_dtype */
+} ragged_grad_tensor;
+int ragged_grad_plan(const ragged_grad_tensor* tensors, int n, void* table, int64_t capacity, int64_t* chunks);
+int ragged_grad_clip(const void* table, int64_t chunks, float scale, float max_norm, void* workspace, double* norm, void* stream);
 
 /*
  * ragged_noop -- enqueue an empty kernel of `grid` work-groups of 256 threads on `stream`.

@@ -22,7 +22,9 @@ _DTYPE_CODE = {torch.float16: RAGGED_F16, torch.bfloat16: RAGGED_BF16, torch.flo
 
 EXPORTS = ("ragged_pack", "ragged_attn", "ragged_attn_strided", "ragged_attn_checked", "ragged_attn_padded", "ragged_unpack",
            "ragged_repack", "ragged_cls_extract", "ragged_pack_attn_unpack", "ragged_linear", "ragged_layernorm",
-           "ragged_token_scores_l2", "ragged_keep_topk", "ragged_noop", "ragged_status_string", "ragged_version")
+           "ragged_token_scores_l2", "ragged_keep_topk", "ragged_rope", "ragged_rope_frequencies", "ragged_attn_lse",
+           "ragged_attn_backward", "ragged_layernorm_backward_workspace", "ragged_layernorm_backward", "ragged_grad_plan",
+           "ragged_grad_clip", "ragged_noop", "ragged_status_string", "ragged_version")
 
 _lib = None
 
@@ -70,6 +72,23 @@ def load() -> ctypes.CDLL:
         lib.ragged_attn_padded.restype = i32
         lib.ragged_unpack.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, i32, vp]
         lib.ragged_unpack.restype = i32
+        f64 = ctypes.c_double
+        lib.ragged_rope.argtypes = [vp, vp, vp, vp, i64, vp, i32, i32, i32, i64, i64, i64, i64, vp, i64, i32, vp, vp, i32, i32, f32, i32, i32, vp]
+        lib.ragged_rope.restype = i32
+        lib.ragged_rope_frequencies.argtypes = [vp, i32, f64, i32, f64, f64, f64, f64]
+        lib.ragged_rope_frequencies.restype = i32
+        lib.ragged_attn_lse.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i64, i64, f32, i32, vp]
+        lib.ragged_attn_lse.restype = i32
+        lib.ragged_attn_backward.argtypes = [vp] * 10 + [i32, i32, i32, i32, i64, i64, i64, f32, i32, vp]
+        lib.ragged_attn_backward.restype = i32
+        lib.ragged_layernorm_backward_workspace.argtypes = [i64, i32]
+        lib.ragged_layernorm_backward_workspace.restype = i64
+        lib.ragged_layernorm_backward.argtypes = [vp] * 8 + [i64, vp, i32, f32, i32, vp]
+        lib.ragged_layernorm_backward.restype = i32
+        lib.ragged_grad_plan.argtypes = [vp, i32, vp, i64, vp]
+        lib.ragged_grad_plan.restype = i32
+        lib.ragged_grad_clip.argtypes = [vp, i64, f32, f32, vp, vp, vp]
+        lib.ragged_grad_clip.restype = i32
         lib.ragged_noop.argtypes = [i32, vp]
         lib.ragged_noop.restype = i32
         lib.ragged_status_string.argtypes = [i32]
@@ -382,6 +401,203 @@ def ragged_unpack(src, keep, cu_seqlens, gather_idx, out, fill_mode: int, stream
     needs keep (gather_idx may be None)."""
     _check("ragged_unpack",
            _native().ragged_unpack(*_unpack_args(src, keep, cu_seqlens, gather_idx, out, fill_mode, stream)))
+
+
+# ---- training on packed rows ------------------------------------------------------------------------------------------------
+
+_HALF = (torch.float16, torch.bfloat16)
+_ROPE_LAYOUT = {"half": 0, "interleaved": 1}
+_ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def rope_frequencies(pairs: int, base: float = 10000.0, axes: int = 1, scaling: str = "none", factor: float = 1.0,
+                     original_length: float = 0.0, fast: float = 32.0, slow: float = 1.0) -> torch.Tensor:
+    """freqs of ragged_rope as a float64 CPU tensor [pairs]: each of the axes has pairs / axes of them, from 1 down to
+    about 1 / base, scaled for long contexts as ``scaling`` says (include/ragged.h has the formulas)."""
+    if axes < 1 or pairs < 1 or pairs % axes != 0:
+        raise ValueError(f"{pairs} pairs cannot be shared out over {axes} axes")
+    one = torch.empty(pairs // axes, dtype=torch.float64)
+    _check("ragged_rope_frequencies", _native().ragged_rope_frequencies(
+        one.data_ptr(), pairs // axes, float(base), _ROPE_SCALING[scaling], float(factor), float(original_length), float(fast), float(slow)))
+    return one.repeat(axes)
+
+
+def _rope_args(q, k, q_out, k_out, coords, freqs, index, layout, amplitude, inverse, rows_dev, stream):
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out come together")
+    qp, qs = _token_rows(q, "q", _HALF, None)
+    qop, qos = _token_rows(q_out, "q_out", q.dtype, q.shape)
+    rows, hq, d = q.shape
+    kp = kop = None
+    hk = ks = kos = 0
+    if k is not None:
+        kp, ks = _token_rows(k, "k", q.dtype, None)
+        kop, kos = _token_rows(k_out, "k_out", q.dtype, k.shape)
+        hk = k.shape[1]
+        if k.shape[0] != rows or k.shape[2] != d:
+            raise ValueError(f"k has shape {tuple(k.shape)}, expected [{rows}, heads, {d}]")
+    if coords.dim() != 2:
+        raise ValueError("coords must be [n, axes]")
+    return (qp, kp, qop, kop, rows, _rows_dev(rows_dev), hq, hk, d, qs, ks, qos, kos, _dev(coords, "coords", torch.float32),
+            coords.shape[0], coords.shape[1], None if index is None else _dev(index, "index", torch.int32, (rows,)),
+            _dev(freqs, "freqs", torch.float64), freqs.numel(), _ROPE_LAYOUT[layout], float(amplitude), int(bool(inverse)),
+            _DTYPE_CODE[q.dtype], _stream(stream))
+
+
+def ragged_rope(q, k, q_out, k_out, coords, freqs, index=None, layout: str = "half", amplitude: float = 1.0, inverse: bool = False,
+                rows_dev=None, stream=None) -> None:
+    """Rotary positions of q [rows,Hq,D] and k [rows,Hk,D] (or None) into q_out, k_out (which may be q, k); token strides as for
+    ragged_attn_strided.  coords [n,axes] float32, freqs [pairs] float64, index [rows] int32: row r is at coords[index[r] mod n]
+    (index None: coords[r mod n])."""
+    _check("ragged_rope", _native().ragged_rope(
+        *_rope_args(q, k, q_out, k_out, coords, freqs, index, layout, amplitude, inverse, rows_dev, stream)))
+
+
+def prepare_rope(q, k, q_out, k_out, coords, freqs, index=None, layout: str = "half", amplitude: float = 1.0, inverse: bool = False,
+                 rows_dev=None, stream=None) -> "Prepared":
+    return Prepared("ragged_rope", load().ragged_rope,
+                    _rope_args(q, k, q_out, k_out, coords, freqs, index, layout, amplitude, inverse, rows_dev, stream),
+                    (q, k, q_out, k_out, coords, freqs, index, rows_dev))
+
+
+def _same_stride(*tensors):
+    """(pointers, token stride) of [rows, H, D] views that share shape, dtype and token stride."""
+    first = tensors[0][0]
+    got = [_token_rows(t, name, _HALF if t is first else first.dtype, first.shape) for t, name in tensors]
+    if len({s for _, s in got}) != 1:
+        raise ValueError(f"{', '.join(n for _, n in tensors)} must share their token stride")
+    return [p for p, _ in got], int(got[0][1])
+
+
+def _attn_lse_args(q, k, v, o, lse, cu_seqlens, max_seqlen, scale, stream):
+    (qp, kp, vp), in_tok = _same_stride((q, "q"), (k, "k"), (v, "v"))
+    op, out_tok = _token_rows(o, "o", q.dtype, q.shape)
+    rows, H, D = q.shape
+    return (qp, kp, vp, op, _dev(lse, "lse", torch.float32, (rows, H)), _dev(cu_seqlens, "cu_seqlens", torch.int32),
+            cu_seqlens.shape[0] - 1, int(max_seqlen), H, D, in_tok, int(out_tok), float(scale), _DTYPE_CODE[q.dtype], _stream(stream))
+
+
+def ragged_attn_lse(q, k, v, o, lse, cu_seqlens, max_seqlen: int, scale: float, stream=None) -> None:
+    """ragged_attn_strided (o of the inputs' dtype) that also writes lse [rows,H] float32 for ragged_attn_backward."""
+    _check("ragged_attn_lse", _native().ragged_attn_lse(*_attn_lse_args(q, k, v, o, lse, cu_seqlens, max_seqlen, scale, stream)))
+
+
+def prepare_attn_lse(q, k, v, o, lse, cu_seqlens, max_seqlen: int, scale: float, stream=None) -> "Prepared":
+    return Prepared("ragged_attn_lse", load().ragged_attn_lse, _attn_lse_args(q, k, v, o, lse, cu_seqlens, max_seqlen, scale, stream),
+                    (q, k, v, o, lse, cu_seqlens))
+
+
+def _attn_backward_args(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen, scale, stream):
+    (qp, kp, vp), in_tok = _same_stride((q, "q"), (k, "k"), (v, "v"))
+    (op, dop), out_tok = _same_stride((o, "o"), (d_o, "d_o"))
+    (dqp, dkp, dvp), grad_tok = _same_stride((dq, "dq"), (dk, "dk"), (dv, "dv"))
+    for t, name in ((o, "o"), (dq, "dq")):
+        if t.dtype != q.dtype or t.shape != q.shape:
+            raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, expected {tuple(q.shape)} {q.dtype}")
+    rows, H, D = q.shape
+    return (qp, kp, vp, op, dop, _dev(lse, "lse", torch.float32, (rows, H)), dqp, dkp, dvp, _dev(cu_seqlens, "cu_seqlens", torch.int32),
+            cu_seqlens.shape[0] - 1, int(max_seqlen), H, D, in_tok, out_tok, grad_tok, float(scale), _DTYPE_CODE[q.dtype], _stream(stream))
+
+
+def ragged_attn_backward(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen: int, scale: float, stream=None) -> None:
+    """Gradients dq, dk, dv of ragged_attn_lse's q, k, v from its output o, that output's gradient d_o and lse.  q, k, v share
+    a token stride, o and d_o share one, dq, dk, dv share one."""
+    _check("ragged_attn_backward", _native().ragged_attn_backward(
+        *_attn_backward_args(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen, scale, stream)))
+
+
+def prepare_attn_backward(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen: int, scale: float, stream=None) -> "Prepared":
+    return Prepared("ragged_attn_backward", load().ragged_attn_backward,
+                    _attn_backward_args(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen, scale, stream),
+                    (q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens))
+
+
+def layernorm_backward_workspace(rows: int, C: int) -> int:
+    """Bytes of workspace that ragged_layernorm_backward needs for up to `rows` rows of width C."""
+    need = int(load().ragged_layernorm_backward_workspace(int(rows), int(C)))
+    if need == 0:
+        raise ValueError(f"{rows} rows of width {C} are not supported")
+    return need
+
+
+def _layernorm_backward_args(x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad, rows_dev, eps, stream):
+    rows, C = x.shape
+    need = layernorm_backward_workspace(rows, C)
+    if workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"workspace has {workspace.numel() * workspace.element_size()} bytes, {need} are needed")
+    return (_dev(x, "x", _HALF), _dev(gamma, "gamma", x.dtype, (C,)), _dev(dy, "dy", x.dtype, (rows, C)),
+            None if residual_grad is None else _dev(residual_grad, "residual_grad", x.dtype, (rows, C)), _dev(dx, "dx", x.dtype, (rows, C)),
+            _dev(dgamma, "dgamma", torch.float32, (C,)), _dev(dbeta, "dbeta", torch.float32, (C,)), _dev(workspace, "workspace"), rows,
+            _rows_dev(rows_dev), C, float(eps), _DTYPE_CODE[x.dtype], _stream(stream))
+
+
+def ragged_layernorm_backward(x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad=None, rows_dev=None, eps: float = 1e-6,
+                              stream=None) -> None:
+    """Gradients of ragged_layernorm over the first min(rows, *rows_dev) rows: dx [rows,C] (+ residual_grad), dgamma, dbeta [C]
+    float32.  workspace: layernorm_backward_workspace(rows, C) bytes."""
+    _check("ragged_layernorm_backward", _native().ragged_layernorm_backward(
+        *_layernorm_backward_args(x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad, rows_dev, eps, stream)))
+
+
+def prepare_layernorm_backward(x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad=None, rows_dev=None, eps: float = 1e-6,
+                               stream=None) -> "Prepared":
+    return Prepared("ragged_layernorm_backward", load().ragged_layernorm_backward,
+                    _layernorm_backward_args(x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad, rows_dev, eps, stream),
+                    (x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad, rows_dev))
+
+
+GRAD_WORKSPACE, GRAD_CHUNK_BYTES = 16384, 32
+
+
+class _GradTensor(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("numel", ctypes.c_int64), ("src_dt", ctypes.c_int32),
+                ("dst_dt", ctypes.c_int32)]
+
+
+class GradPlan:
+    """The tensors of one ragged_grad_clip, laid out once: ``grads`` and, for each, where the clipped values go (``outs``: a
+    tensor of the same shape and of the same dtype or float32, the gradient itself, or None for a tensor that counts for the norm
+    only; outs None: in place).  Holds the table, a workspace and the tensors, which must stay in place.  Calls with one plan
+    must not run at the same time (on other streams, in other captured graphs): they share its workspace."""
+
+    def __init__(self, grads, outs=None):
+        grads = list(grads)
+        outs = grads if outs is None else list(outs)
+        if not grads or len(outs) != len(grads):
+            raise ValueError(f"{len(grads)} gradients and {len(outs)} outputs")
+        dtypes = (torch.float32, *_HALF)
+        entries = (_GradTensor * len(grads))()
+        for e, g, o in zip(entries, grads, outs):
+            e.src, e.numel, e.src_dt = _dev(g, "grad", dtypes), g.numel(), _DTYPE_CODE[g.dtype]
+            if g.device != grads[0].device or (o is not None and o.device != grads[0].device):
+                raise ValueError("all tensors must be on one device")
+            if o is not None:
+                e.dst, e.dst_dt = _dev(o, "out", (g.dtype, torch.float32), tuple(g.shape)), _DTYPE_CODE[o.dtype]
+        chunks = ctypes.c_int64()
+        plan = lambda table, size: _check("ragged_grad_plan", _native().ragged_grad_plan(
+            ctypes.addressof(entries), len(grads), table, size, ctypes.addressof(chunks)))
+        plan(None, 0)
+        self.chunks = chunks.value
+        host = torch.empty(max(1, self.chunks) * GRAD_CHUNK_BYTES, dtype=torch.uint8)
+        plan(host.data_ptr(), host.numel())
+        self.table = host.to(grads[0].device)
+        self.workspace = torch.empty(GRAD_WORKSPACE, dtype=torch.uint8, device=grads[0].device)
+        self.tensors = (grads, outs)
+
+
+def _grad_clip_args(plan, norm, max_norm, scale, stream):
+    return (plan.table.data_ptr(), plan.chunks, float(scale), float(max_norm), plan.workspace.data_ptr(),
+            _dev(norm, "norm", torch.float64, (1,)), _stream(stream))
+
+
+def ragged_grad_clip(plan: GradPlan, norm, max_norm: float, scale: float = 1.0, stream=None) -> None:
+    """norm [1] float64 = |scale| * l2 norm over the plan's gradients; its outputs = gradient * scale * min(1, max_norm / (norm + 1e-6)).
+    A norm that is not finite clips nothing."""
+    _check("ragged_grad_clip", _native().ragged_grad_clip(*_grad_clip_args(plan, norm, max_norm, scale, stream)))
+
+
+def prepare_grad_clip(plan: GradPlan, norm, max_norm: float, scale: float = 1.0, stream=None) -> "Prepared":
+    return Prepared("ragged_grad_clip", load().ragged_grad_clip, _grad_clip_args(plan, norm, max_norm, scale, stream), (plan, norm))
 
 
 _UNTYPED = None

@@ -15,7 +15,8 @@ ROOT = PKG.parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libragged_hip.so"
 BUILD_DIR = PKG / "_build"
-SOURCES = ["ragged_api.hip", "pack_unpack.hip", "attn.hip", "linear.hip", "linear_f16.hip", "linear_bf16.hip", "mask.hip"]
+SOURCES = ["ragged_api.hip", "pack_unpack.hip", "attn.hip", "linear.hip", "linear_f16.hip", "linear_bf16.hip", "mask.hip",
+           "rope.hip", "attn_backward.hip", "layernorm_backward.hip", "grad_clip.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

@@ -40,6 +40,7 @@
 // together) and P V is two MFMAs; V stays exact.  The path is not MFMA-bound at ViT lengths.
 #include <type_traits>
 
+#include "attn_parts.h"
 #include "common.h"
 #include "mask_prefix.h"
 #include "mfma_lds.h"
@@ -47,8 +48,6 @@
 namespace ragged {
 namespace {
 
-constexpr int kHeadDim = 64;
-constexpr int kBN = 64;                 // keys per K/V tile
 // Work-group shape.  Measured on the dense layer (B=64, n=197) and the pruned batches: four wavefronts with a ring of two
 // tiles (32 KB, four work-groups per CU) is the fastest; deeper rings (3, 4) lose resident wavefronts and gain nothing,
 // eight-wavefront groups tie on dense batches and lose on short sequences (577 tokens, B=32: 78 against 72 us).
@@ -56,7 +55,6 @@ constexpr int kRing = 2;                // K/V tiles resident in LDS per work-gr
 constexpr int kAttnWaves = 4;           // wavefronts per work-group
 constexpr int kAttnThreads = kWaveSize * kAttnWaves;
 constexpr int kAttnOcc = 4;             // work-groups per CU aimed at
-constexpr int kTileBytes = kBN * kHeadDim * 2;   // one K or one V tile: 8 KB
 // A sequence's LAST tile takes a tail of up to 16 keys along (n = 64k + 1 .. 64k + 16, k >= 2): 80 keys in one
 // pass instead of a pass of its own for a handful of keys -- ViT lengths are 64k + 1 before pruning (197, 577).
 // (Not for k = 1: the first tile of a sequence has a form of its own, and a second copy of it for 80 keys
@@ -64,11 +62,9 @@ constexpr int kTileBytes = kBN * kHeadDim * 2;   // one K or one V tile: 8 KB
 // The tail's K rows and V rows live behind the ring.
 constexpr int kExtraRows = 16;
 constexpr int kExtraBytes = 2 * kExtraRows * kHeadDim * 2;   // K rows, then V rows: 4 KB
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazyLog2 = 8.0f;       // probabilities stay below 2^8 between rescales
 constexpr int kSplitMaxGroups = 256;    // launches of at most this many 64-row q-tiles split the keys over the wavefronts
 constexpr int kMaxGatherTokens = 1536;  // tokens per image the gather-on-load variant can index in LDS
-constexpr int kMaxGridYZ = 65535;       // HIP's limit on the second and third grid dimension
 // Dispatch in phases (the order is described at the kernel).
 constexpr int kPhasePairs = 128;        // pairs of a dispatch batch
 constexpr int kPhaseTiles = 5;          // q-tiles of a phase; smaller bounds have one phase
@@ -124,63 +120,6 @@ __device__ __forceinline__ void pv_block(BF16, const uint4 (&vt)[4], const float
     l = BF16::mfma(ones, lo, l);
 }
 
-// Store 16 consecutive head-dim elements of one output row.
-__device__ __forceinline__ void store16(_Float16* dst, const float (&v)[16]) {
-    f16x8 a, b;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) { a[e] = (_Float16)v[e]; b[e] = (_Float16)v[8 + e]; }
-    reinterpret_cast<uint4*>(dst)[0] = __builtin_bit_cast(uint4, a);
-    reinterpret_cast<uint4*>(dst)[1] = __builtin_bit_cast(uint4, b);
-}
-__device__ __forceinline__ void store16(__bf16* dst, const float (&v)[16]) {
-    bf16x8 a, b;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) { a[e] = (__bf16)v[e]; b[e] = (__bf16)v[8 + e]; }
-    reinterpret_cast<uint4*>(dst)[0] = __builtin_bit_cast(uint4, a);
-    reinterpret_cast<uint4*>(dst)[1] = __builtin_bit_cast(uint4, b);
-}
-__device__ __forceinline__ void store16(float* dst, const float (&v)[16]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        reinterpret_cast<float4*>(dst)[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
-}
-
-// Store 4 consecutive head-dim elements of one output row.
-__device__ __forceinline__ void store4(_Float16* dst, const float (&v)[4]) {
-    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-    const f16x4 a = {(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
-    *reinterpret_cast<uint2*>(dst) = __builtin_bit_cast(uint2, a);
-}
-__device__ __forceinline__ void store4(__bf16* dst, const float (&v)[4]) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    const bf16x4 a = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-    *reinterpret_cast<uint2*>(dst) = __builtin_bit_cast(uint2, a);
-}
-__device__ __forceinline__ void store4(float* dst, const float (&v)[4]) {
-    *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
-}
-
-// Reductions over the four lanes that share a query (l, l^16, l^32, l^48) with the gfx950 lane-swap
-// instructions (pure VALU, no LDS round trip).  permlane32_swap(a, b) returns {a.lo|b.lo, a.hi|b.hi}
-// (32-lane halves); permlane16_swap(a, b) returns {a.row0,b.row0,a.row2,b.row2} and
-// {a.row1,b.row1,a.row3,b.row3} (16-lane rows).  With b a copy of a, combining the two results
-// reduces across the halves, then across the rows.  The copy is made through an opaque move so the
-// two operands can never be folded into one register (the instruction swaps its operands in place).
-__device__ __forceinline__ unsigned opaque_copy(unsigned x) {
-    unsigned y;
-    asm volatile("v_mov_b32 %0, %1" : "=v"(y) : "v"(x));
-    return y;
-}
-__device__ __forceinline__ float as_f32(unsigned u) { return __builtin_bit_cast(float, u); }
-__device__ __forceinline__ unsigned as_u32(float f) { return __builtin_bit_cast(unsigned, f); }
-__device__ __forceinline__ float quad_max(float x) {
-    const auto a = __builtin_amdgcn_permlane32_swap(as_u32(x), opaque_copy(as_u32(x)), false, false);
-    const unsigned a0 = a[0], a1 = a[1];
-    x = fmaxf(as_f32(a0), as_f32(a1));
-    const auto b = __builtin_amdgcn_permlane16_swap(as_u32(x), opaque_copy(as_u32(x)), false, false);
-    const unsigned b0 = b[0], b1 = b[1];
-    return fmaxf(as_f32(b0), as_f32(b1));
-}
 // One K/V tile (already in LDS) against this wavefront's 16 queries: S^T = K Q^T, online-softmax
 // update, O^T += V^T P^T.  NT = 16-key subtiles present in the tile (1..4, or 5: a full tile plus the tail
 // subtile kept behind the ring, whose K / transposed V operand addresses are ek_a0 / ev_a0 -- the second
@@ -194,12 +133,14 @@ __device__ __forceinline__ float quad_max(float x) {
 // FIRST: the sequence's first tile.  The running maximum is this tile's maximum and the accumulators are
 // written, not updated: no rescaling, no zero-initialised registers.  (The general form would reach the same
 // values through alpha = exp2(-inf) = 0 and accumulators cleared beforehand.)
-template <typename In, int NT, bool MASK, bool FIRST>
+// LSE: l_sum is this lane's share of the row sum in fp32, of the probabilities before they are rounded for P V (it follows the
+// running maximum as l_acc does; the output is still divided by l_acc, so it is the same with and without LSE).
+template <typename In, int NT, bool MASK, bool FIRST, bool LSE>
 __device__ __forceinline__ void tile_update(uint32_t k_a0, uint32_t k_a1, uint32_t v_a0, uint32_t v_a1,
                                             uint32_t ek_a0, uint32_t ev_a0,
                                             const typename In::vec8 (&q_frag)[2], int rem, int g,
                                             float scale_log2e, float& m_run, f32x4& l_acc,
-                                            f32x4 (&o_acc)[4]) {
+                                            f32x4 (&o_acc)[4], float& l_sum) {
     typedef typename In::vec8 vec8;
     // -------- S^T = K Q^T : NT 16-key subtiles, two k-steps of 32 head-dim elements
     f32x4 st[NT];
@@ -233,6 +174,7 @@ __device__ __forceinline__ void tile_update(uint32_t k_a0, uint32_t k_a1, uint32
         const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
         l_acc *= alpha;
+        if (LSE) l_sum *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) o_acc[dt] *= alpha;
     }
@@ -244,6 +186,12 @@ __device__ __forceinline__ void tile_update(uint32_t k_a0, uint32_t k_a1, uint32
             if (MASK && kt == NT - 1) p = (r < last_valid) ? p : 0.f;
             st[kt][r] = p;
         }
+    if (LSE) {
+        float sum = FIRST ? 0.f : l_sum;
+#pragma unroll
+        for (int kt = 0; kt < NT; ++kt) sum += (st[kt][0] + st[kt][1]) + (st[kt][2] + st[kt][3]);
+        l_sum = sum;
+    }
     // -------- O^T += V^T P^T : 32-key blocks x four 16-row head-dim tiles (NT 1 or 3: zero upper half)
     constexpr int kBlocks = NT == 5 ? 2 : (NT + 1) / 2;
 #pragma unroll
@@ -283,23 +231,23 @@ __device__ __forceinline__ void tile_update(uint32_t k_a0, uint32_t k_a1, uint32
 // A tile of `rem` remaining keys at LDS address tile0: full tiles take the unmasked form, a tail is specialised
 // on its number of 16-key subtiles.  k_rel0 / v_rel0: this lane's operand offsets inside a tile; ext_tile: a last
 // tile of 65..80 keys whose rows 64.. are kept behind the ring at LDS address extra0 (EXT: the kernel form has them).
-template <typename In, bool FIRST, bool EXT>
+template <typename In, bool FIRST, bool EXT, bool LSE>
 __device__ __forceinline__ void tile_any(int rem, bool ext_tile, uint32_t tile0, uint32_t extra0, uint32_t k_rel0, uint32_t v_rel0,
                                          const typename In::vec8 (&q_frag)[2], int g, float scale_log2e,
-                                         float& m_run, f32x4& l_acc, f32x4 (&o_acc)[4]) {
+                                         float& m_run, f32x4& l_acc, f32x4 (&o_acc)[4], float& l_sum) {
     const uint32_t k_a0 = tile0 + k_rel0, k_a1 = tile0 + (k_rel0 ^ 16u);
     const uint32_t v_a0 = tile0 + v_rel0, v_a1 = tile0 + (v_rel0 ^ 16u);
     const uint32_t ek_a0 = extra0 + k_rel0, ev_a0 = extra0 + kExtraBytes / 2 + (v_rel0 - kTileBytes);
     if (EXT && ext_tile) {
-        tile_update<In, 5, true, FIRST>(k_a0, k_a1, v_a0, v_a1, ek_a0, ev_a0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc);
+        tile_update<In, 5, true, FIRST, LSE>(k_a0, k_a1, v_a0, v_a1, ek_a0, ev_a0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum);
     } else if (rem >= kBN) {
-        tile_update<In, 4, false, FIRST>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc);
+        tile_update<In, 4, false, FIRST, LSE>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum);
     } else {
         switch ((rem + 15) >> 4) {
-            case 1: tile_update<In, 1, true, FIRST>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc); break;
-            case 2: tile_update<In, 2, true, FIRST>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc); break;
-            case 3: tile_update<In, 3, true, FIRST>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc); break;
-            default: tile_update<In, 4, true, FIRST>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc); break;
+            case 1: tile_update<In, 1, true, FIRST, LSE>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum); break;
+            case 2: tile_update<In, 2, true, FIRST, LSE>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum); break;
+            case 3: tile_update<In, 3, true, FIRST, LSE>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum); break;
+            default: tile_update<In, 4, true, FIRST, LSE>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum); break;
         }
     }
 }
@@ -356,6 +304,7 @@ struct StepArgs {
     int64_t cap_rows;
     int32_t* flags;             // MODE kPacked only, may be null: bit 0 is set when some n_i > max_seqlen
     int max_seqlen;
+    float* lse;                 // [rows, H], LSE only: ln of the row sums of exp(scale q.k)
 };
 
 // SPLIT (small launches, where a work-group has a CU to itself and the path is a chain of latencies):
@@ -364,7 +313,9 @@ struct StepArgs {
 //   arithmetic on them; the four partial results (running maximum, row sum, accumulators) are merged
 //   through LDS at the end, each wavefront finishing four of the sixteen head-dim elements a lane owns.
 //   A sequence of up to 256 tokens then costs one tile time plus the merge instead of up to four.
-template <typename In, typename OutT, int MODE, bool SPLIT>
+//
+// LSE (MODE kPacked): the kernel also writes step.lse for the backward pass; o is the same, bit for bit.
+template <typename In, typename OutT, int MODE, bool SPLIT, bool LSE>
 __global__ __launch_bounds__(kAttnThreads, SPLIT ? 2 : kAttnOcc)
 void attn_kernel(const void* __restrict__ index, int n_tok, int fill_mode, int H, uint32_t h_magic, int pairs,
                  int group_phase, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, int tok32,
@@ -636,6 +587,7 @@ void attn_kernel(const void* __restrict__ index, int n_tok, int fill_mode, int H
     // settles on a schedule of that kernel that is 4 % slower on the headline batch)
     constexpr bool PEEL = MODE != kStep;
     float m_run;
+    float l_sum = 0.f;                      // LSE
     f32x4 l_acc;
     f32x4 o_acc[4];
     if (!PEEL) {
@@ -654,17 +606,21 @@ void attn_kernel(const void* __restrict__ index, int n_tok, int fill_mode, int H
                 reinterpret_cast<uint4*>(step.packed + ((int64_t)s + j) * tok + head_off)[tid & 7] = x_raw[i];
         }
     };
+    // LSE: maximum (log2 domain) and full row sum of a query -> natural logarithm; one lane of the four that share the query writes
+    auto store_lse = [&](float top, float sum) {
+        if (g == 0) step.lse[((int64_t)s + q_row) * H + h] = (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+    };
     if (SPLIT) {
         // ---- this wavefront's tiles wave, wave + 4, ...: its own slot, its own loads, no barrier
         const uint32_t tile0 = ring0 + wave * 2 * kTileBytes;
         if (wave < tiles) {
             wait_vm<0>();                   // the tile has landed (the loads were this wavefront's own)
             // its results depend on every LDS read of the tile: the slot is free after it
-            tile_any<In, PEEL, false>(n - wave * kBN, false, tile0, 0, k_rel0, v_rel0, q_frag, g, scale_log2e, m_run, l_acc, o_acc);
+            tile_any<In, PEEL, false, LSE>(n - wave * kBN, false, tile0, 0, k_rel0, v_rel0, q_frag, g, scale_log2e, m_run, l_acc, o_acc, l_sum);
             for (int t = wave + WAVES; t < tiles; t += WAVES) {
                 issue_own(t);
                 wait_vm<0>();
-                tile_any<In, false, false>(n - t * kBN, false, tile0, 0, k_rel0, v_rel0, q_frag, g, scale_log2e, m_run, l_acc, o_acc);
+                tile_any<In, false, false, LSE>(n - t * kBN, false, tile0, 0, k_rel0, v_rel0, q_frag, g, scale_log2e, m_run, l_acc, o_acc, l_sum);
             }
         } else {                            // no tile for this wavefront: it contributes nothing to the merge
             m_run = -INFINITY;
@@ -673,8 +629,10 @@ void attn_kernel(const void* __restrict__ index, int n_tok, int fill_mode, int H
             for (int dt = 0; dt < 4; ++dt) o_acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         if (MODE == kStep) store_packed_rows();
+        if (LSE) l_sum = quad_sum(l_sum);
         if (tiles == 1) {                   // a single tile: wavefront 0 holds the whole result, nothing to merge
             if (wave == 0 && q_row < n) {
+                if (LSE) store_lse(m_run, l_sum);
                 const bool row_fits = MODE != kStep || (int64_t)s + q_row < step.cap_rows;
                 const float inv = 1.0f / l_acc[0];
                 float out16[16];
@@ -692,6 +650,7 @@ void attn_kernel(const void* __restrict__ index, int n_tok, int fill_mode, int H
         float* const part = reinterpret_cast<float*>(ring) + wave * (2 * kTileBytes / 4);
         part[lane] = m_run;
         part[kWaveSize + lane] = l_acc[0];
+        if (LSE) part[18 * kWaveSize + lane] = l_sum;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -706,15 +665,17 @@ void attn_kernel(const void* __restrict__ index, int n_tok, int fill_mode, int H
                 m_w[w2] = all[w2 * (2 * kTileBytes / 4) + lane];
                 m_all = fmaxf(m_all, m_w[w2]);  // finite: wavefront 0 always has tile 0
             }
-            float l_all = 0.f, o4[4] = {0.f, 0.f, 0.f, 0.f};
+            float l_all = 0.f, sum_all = 0.f, o4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w2 = 0; w2 < WAVES; ++w2) {
                 const float f = __builtin_amdgcn_exp2f(m_w[w2] - m_all);
                 const float* pw = all + w2 * (2 * kTileBytes / 4);
                 l_all = __builtin_fmaf(f, pw[kWaveSize + lane], l_all);
+                if (LSE) sum_all = __builtin_fmaf(f, pw[18 * kWaveSize + lane], sum_all);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o4[r] = __builtin_fmaf(f, pw[(2 + 4 * wave + r) * kWaveSize + lane], o4[r]);
             }
+            if (LSE && wave == 0) store_lse(m_all, sum_all);
             const float inv = 1.0f / l_all;
 #pragma unroll
             for (int r = 0; r < 4; ++r) o4[r] *= inv;
@@ -740,7 +701,7 @@ void attn_kernel(const void* __restrict__ index, int n_tok, int fill_mode, int H
         landed();
         if (tiles > 1) issue(1, 1);
         if (wave_active)
-            tile_any<In, true, false>(n, false, ring0, extra0, k_rel0, v_rel0, q_frag, g, scale_log2e, m_run, l_acc, o_acc);
+            tile_any<In, true, false, LSE>(n, false, ring0, extra0, k_rel0, v_rel0, q_frag, g, scale_log2e, m_run, l_acc, o_acc, l_sum);
         if (tiles > 1) {
             for (int t = 1; t < tiles - 1; ++t) {
                 slot ^= 1;
@@ -748,14 +709,14 @@ void attn_kernel(const void* __restrict__ index, int n_tok, int fill_mode, int H
                 issue(t + 1, slot ^ 1);
                 const uint32_t tile0 = ring0 + slot * 2 * kTileBytes;
                 if (wave_active)
-                    tile_update<In, 4, false, false>(tile0 + k_rel0, tile0 + (k_rel0 ^ 16u), tile0 + v_rel0, tile0 + (v_rel0 ^ 16u), 0, 0,
-                                                     q_frag, kBN, g, scale_log2e, m_run, l_acc, o_acc);
+                    tile_update<In, 4, false, false, LSE>(tile0 + k_rel0, tile0 + (k_rel0 ^ 16u), tile0 + v_rel0, tile0 + (v_rel0 ^ 16u), 0, 0,
+                                                     q_frag, kBN, g, scale_log2e, m_run, l_acc, o_acc, l_sum);
             }
             slot ^= 1;
             landed();
             if (wave_active)
-                tile_any<In, false, EXT>(n - (tiles - 1) * kBN, rides, ring0 + slot * 2 * kTileBytes, extra0, k_rel0, v_rel0,
-                                         q_frag, g, scale_log2e, m_run, l_acc, o_acc);
+                tile_any<In, false, EXT, LSE>(n - (tiles - 1) * kBN, rides, ring0 + slot * 2 * kTileBytes, extra0, k_rel0, v_rel0,
+                                         q_frag, g, scale_log2e, m_run, l_acc, o_acc, l_sum);
         }
     } else {
         // kStep: one loop with every form of a tile.  Its launches are mostly of short sequences, for which the code above is
@@ -770,15 +731,15 @@ void attn_kernel(const void* __restrict__ index, int n_tok, int fill_mode, int H
                 const uint32_t v_a0 = tile0 + v_rel0, v_a1 = tile0 + (v_rel0 ^ 16u);
                 const uint32_t ek_a0 = extra0 + k_rel0, ev_a0 = extra0 + kExtraBytes / 2 + (v_rel0 - kTileBytes);
                 if (t == ride_tile) {
-                    tile_update<In, 5, true, false>(k_a0, k_a1, v_a0, v_a1, ek_a0, ev_a0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc);
+                    tile_update<In, 5, true, false, LSE>(k_a0, k_a1, v_a0, v_a1, ek_a0, ev_a0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum);
                 } else if (rem >= kBN) {
-                    tile_update<In, 4, false, false>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc);
+                    tile_update<In, 4, false, false, LSE>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum);
                 } else {
                     switch ((rem + 15) >> 4) {
-                        case 1: tile_update<In, 1, true, false>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc); break;
-                        case 2: tile_update<In, 2, true, false>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc); break;
-                        case 3: tile_update<In, 3, true, false>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc); break;
-                        default: tile_update<In, 4, true, false>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc); break;
+                        case 1: tile_update<In, 1, true, false, LSE>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum); break;
+                        case 2: tile_update<In, 2, true, false, LSE>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum); break;
+                        case 3: tile_update<In, 3, true, false, LSE>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum); break;
+                        default: tile_update<In, 4, true, false, LSE>(k_a0, k_a1, v_a0, v_a1, 0, 0, q_frag, rem, g, scale_log2e, m_run, l_acc, o_acc, l_sum); break;
                     }
                 }
             }
@@ -799,7 +760,9 @@ void attn_kernel(const void* __restrict__ index, int n_tok, int fill_mode, int H
 
     // ---- normalise and store: this lane owns d = 16g + 4dt + r of its query
     const bool row_fits = MODE != kStep || (int64_t)s + q_row < step.cap_rows;
+    if (LSE && wave_active) l_sum = quad_sum(l_sum);
     if (wave_active && q_row < n) {
+        if (LSE) store_lse(m_run, l_sum);
         const float inv = 1.0f / l_acc[0];
         float out16[16];
 #pragma unroll
@@ -812,7 +775,7 @@ void attn_kernel(const void* __restrict__ index, int n_tok, int fill_mode, int H
     }
 }
 
-template <typename In, typename OutT, int MODE>
+template <typename In, typename OutT, int MODE, bool LSE = false>
 hipError_t launch_typed(const void* q, const void* k, const void* v, void* o,
                         const int32_t* cu_seqlens, const uint8_t* keep, int n_tok, int fill_mode,
                         int B, int max_seqlen, int H, int64_t in_tok, int64_t out_tok, float scale,
@@ -846,7 +809,7 @@ hipError_t launch_typed(const void* q, const void* k, const void* v, void* o,
     const int batches = phased ? (int)phase_batches : (pairs + group - 1) / group;
     if (q_tiles > kMaxGridYZ || batches > kMaxGridYZ || in_tok > INT32_MAX || out_tok > INT32_MAX)
         return hipErrorInvalidValue;                            // (the C ABI layer has refused these already)
-    const hipError_t err = launch_kernel(split ? attn_kernel<In, OutT, MODE, true> : attn_kernel<In, OutT, MODE, false>,
+    const hipError_t err = launch_kernel(split ? attn_kernel<In, OutT, MODE, true, LSE> : attn_kernel<In, OutT, MODE, false, LSE>,
                        dim3(group, phased ? phase_tiles : q_tiles, batches), dim3(kAttnThreads), stream,
                        MODE == kPacked ? static_cast<const void*>(cu_seqlens) : static_cast<const void*>(keep),
                        n_tok, fill_mode, H, div_magic((uint32_t)H), pairs, phased ? -phase_tiles : group,
@@ -884,6 +847,18 @@ hipError_t launch_attn(const void* q, const void* k, const void* v, void* o,
                                in_dt, out_dt, extra, stream);
 }
 
+hipError_t launch_attn_lse(const void* q, const void* k, const void* v, void* o, float* lse, const int32_t* cu_seqlens, int B, int max_seqlen,
+                           int H, int64_t in_tok, int64_t out_tok, float scale, ragged_dtype dt, hipStream_t stream) {
+    StepArgs extra{};
+    extra.max_seqlen = max_seqlen;
+    extra.lse = lse;
+    if (dt == RAGGED_F16)
+        return launch_typed<F16, _Float16, kPacked, true>(q, k, v, o, cu_seqlens, nullptr, 0, 0, B, max_seqlen, H, in_tok, out_tok, scale,
+                                                          extra, stream);
+    return launch_typed<BF16, __bf16, kPacked, true>(q, k, v, o, cu_seqlens, nullptr, 0, 0, B, max_seqlen, H, in_tok, out_tok, scale, extra,
+                                                     stream);
+}
+
 int attn_padded_max_tokens() { return kMaxGatherTokens; }
 
 hipError_t launch_attn_padded(const void* q, const void* k, const void* v, void* o, const uint8_t* keep,
@@ -900,7 +875,7 @@ hipError_t launch_step(const void* x, const uint8_t* keep, const void* q, const 
                        hipStream_t stream) {
     const int64_t tok = (int64_t)H * kHeadDim;
     const StepArgs step{static_cast<const uint16_t*>(x), static_cast<uint16_t*>(packed),
-                        static_cast<uint16_t*>(out), cu_seqlens, gather_idx, cap_rows, nullptr, 0};
+                        static_cast<uint16_t*>(out), cu_seqlens, gather_idx, cap_rows, nullptr, 0, nullptr};
     if (dt == RAGGED_F16)
         return launch_typed<F16, _Float16, kStep>(q, k, v, o, nullptr, keep, N, fill_mode, B, N, H, tok, tok, scale,
                                                   step, stream);

@@ -75,6 +75,25 @@ hipError_t launch_token_scores_l2(const void* x, int64_t rows, int C, ragged_dty
 hipError_t launch_keep_topk(const double* scores, int B, int N, int k, uint8_t* keep, hipStream_t stream);
 int keep_topk_max_tokens();
 int attn_padded_max_tokens();
+hipError_t launch_rope(const void* q, const void* k, void* q_out, void* k_out, int rows_cap, const int32_t* rows_dev, int Hq, int Hk, int D,
+                       int64_t q_stride, int64_t k_stride, int64_t q_out_stride, int64_t k_out_stride, const float* coords, int n_coords,
+                       int axes, const int32_t* index, const double* freqs, int pairs, int interleaved, float amplitude, int inverse,
+                       ragged_dtype dt, hipStream_t stream);
+// launch_attn that also writes lse [rows, H]; o has the input dtype
+hipError_t launch_attn_lse(const void* q, const void* k, const void* v, void* o, float* lse, const int32_t* cu_seqlens, int B, int max_seqlen,
+                           int H, int64_t in_tok, int64_t out_tok, float scale, ragged_dtype dt, hipStream_t stream);
+hipError_t launch_attn_backward(const void* q, const void* k, const void* v, const void* o, const void* d_o, const float* lse, void* dq, void* dk,
+                                void* dv, const int32_t* cu_seqlens, int B, int max_seqlen, int H, int64_t in_tok, int64_t out_tok,
+                                int64_t grad_tok, float scale, ragged_dtype dt, hipStream_t stream);
+// two kernels: rows, then the sums over the work-groups
+hipError_t launch_layernorm_backward(const void* x, const void* gamma, const void* dy, const void* res, void* dx, float* dgamma, float* dbeta,
+                                     void* workspace, int rows_cap, const int32_t* rows_dev, int C, float eps, ragged_dtype dt,
+                                     hipStream_t stream);
+int64_t layernorm_backward_workspace(int64_t rows_cap, int C);
+// two kernels: sums of squares, then the scaling
+hipError_t launch_grad_clip(const void* table, int chunks, float scale, float max_norm, void* workspace, double* norm, hipStream_t stream);
+int64_t grad_chunks(const ragged_grad_tensor& t);
+void grad_table(const ragged_grad_tensor* tensors, int n, void* table);
 hipError_t launch_noop(int grid, hipStream_t stream);
 
 // Tokens of one image handled by one work-group of the pack / zero-filling unpack kernels.

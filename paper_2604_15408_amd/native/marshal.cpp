@@ -100,6 +100,8 @@ PyMethodDef methods[] = {
     ENTRY(ragged_pack), ENTRY(ragged_attn), ENTRY(ragged_attn_strided), ENTRY(ragged_attn_checked), ENTRY(ragged_attn_padded),
     ENTRY(ragged_unpack), ENTRY(ragged_repack), ENTRY(ragged_cls_extract), ENTRY(ragged_pack_attn_unpack), ENTRY(ragged_linear),
     ENTRY(ragged_layernorm), ENTRY(ragged_token_scores_l2), ENTRY(ragged_keep_topk), ENTRY(ragged_noop),
+    ENTRY(ragged_rope), ENTRY(ragged_rope_frequencies), ENTRY(ragged_attn_lse), ENTRY(ragged_attn_backward), ENTRY(ragged_layernorm_backward),
+    ENTRY(ragged_grad_plan), ENTRY(ragged_grad_clip),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ragged_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,132 @@
+"""GradPlan and ragged_grad_clip against fp64.  Norm: fp64 sums of exact squares, 1e-12.  Outputs: the factor and the product are rounded to
+fp32 (2^-24 each), then to the output's type."""
+import math
+
+import pytest
+import torch
+
+from paper_2604_15408_amd import binding, harness
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+_TYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _norm(grads, scale):
+    return abs(scale) * math.sqrt(math.fsum(float(g.double().square().sum()) for g in grads))
+
+
+def _check(grads, outs, scale, max_norm, norm):
+    want = _norm(grads, scale)
+    assert abs(float(norm) - want) <= 1e-12 * want
+    factor = scale * min(1.0, max_norm / (want + 1e-6))
+    for g, o in zip(grads, outs):
+        if o is None:
+            continue
+        w = g.double() * factor
+        u = torch.finfo(o.dtype).eps / 2
+        assert torch.all((o.double() - w).abs() <= (u + 2.0 ** -22) * w.abs() + (2.0 ** -25 if o.dtype == torch.float16 else 2.0 ** -133)), o.shape
+
+
+def _make(sizes, dtype, seed=0, times=1.0):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    return [(torch.randn(n, generator=gen, device=DEV) * times).to(_TYPES[dtype]) for n in sizes]
+
+
+SIZES = [[1], [0, 3, 7, 8, 9], [16383, 16384, 16385, 5], [200001, 2047, 2048, 2049, 1, 0], [64] * 300]
+
+
+@pytest.mark.parametrize("src,dst", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("f16", "f32"), ("bf16", "f32")])
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: f"{len(s)}of{s[0]}")
+def test_clip(sizes, src, dst):
+    grads = _make(sizes, src, len(sizes))
+    kept = [g.clone() for g in grads]
+    # outputs behind one another, each but the first off by one value: nothing but its own alignment
+    flat = torch.full((sum(sizes) + 2,), 7.0, dtype=_TYPES[dst], device=DEV)
+    outs = list(flat[1:-1].split(sizes))
+    norm = torch.zeros(1, dtype=torch.float64, device=DEV)
+    plan = binding.GradPlan(grads, outs)
+    for max_norm, scale in ((0.5, 1.0), (math.inf, 0.0078125), (1e6, 1.0), (1.0, -2.0)):
+        flat.fill_(7.0)
+        binding.ragged_grad_clip(plan, norm, max_norm, scale)
+        _check(grads, outs, scale, max_norm, norm)
+        assert flat[0] == 7 and flat[-1] == 7
+    assert all(torch.equal(a, b) for a, b in zip(grads, kept))
+    # in place, from tensors that are off by one value as well
+    base = torch.cat([grads[0].new_zeros(1)] + grads)
+    views = list(base[1:].split(sizes))
+    for max_norm in (0.5, 1e6):
+        before = [v.clone() for v in views]
+        binding.prepare_grad_clip(binding.GradPlan(views), norm, max_norm)()
+        _check(before, views, 1.0, max_norm, norm)
+    assert base[0] == 0
+
+
+def test_mixed_types_and_tensors_without_output():
+    grads = _make([5000], "f32", 1) + _make([70000, 33], "bf16", 2) + _make([129], "f16", 3) + [torch.randn(3, 5, 7, device=DEV)]
+    outs = [None, torch.empty(70000, device=DEV), torch.empty(33, dtype=torch.bfloat16, device=DEV), None, torch.empty(3, 5, 7, device=DEV)]
+    norm = torch.zeros(1, dtype=torch.float64, device=DEV)
+    binding.ragged_grad_clip(binding.GradPlan(grads, outs), norm, 1.0)
+    _check(grads, outs, 1.0, 1.0, norm)
+    again = torch.zeros_like(norm)
+    binding.ragged_grad_clip(binding.GradPlan(grads, [None] * 5), again, 1.0)
+    assert torch.equal(norm, again)
+
+
+def test_sizes_of_gradients():
+    """Squares that would overflow or vanish in 32 bits."""
+    norm = torch.zeros(1, dtype=torch.float64, device=DEV)
+    for times in (1e30, 1e-30):
+        g = [torch.full((1000,), times, device=DEV)]
+        out = [torch.empty(1000, device=DEV)]
+        binding.ragged_grad_clip(binding.GradPlan(g, out), norm, 1.0)
+        _check(g, out, 1.0, 1.0, norm)
+    zeros = [torch.zeros(100, device=DEV)]
+    binding.ragged_grad_clip(binding.GradPlan(zeros), norm, 1.0)
+    assert float(norm) == 0 and not zeros[0].any()
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_norms_that_are_not_finite_clip_nothing(bad):
+    grads = _make([20000, 5], "f16", 4)
+    grads[0][19999] = bad
+    outs = [torch.empty_like(g, dtype=torch.float32) for g in grads]
+    norm = torch.zeros(1, dtype=torch.float64, device=DEV)
+    binding.ragged_grad_clip(binding.GradPlan(grads, outs), norm, 0.5, scale=0.25)
+    assert not math.isfinite(float(norm)) and math.isnan(float(norm)) == math.isnan(bad)
+    for g, o in zip(grads, outs):
+        assert torch.equal(torch.nan_to_num(o, nan=3.0), torch.nan_to_num(g.float() * 0.25, nan=3.0))
+
+
+def test_only_empty_tensors():
+    norm = torch.full((1,), 7.0, dtype=torch.float64, device=DEV)
+    binding.ragged_grad_clip(binding.GradPlan([torch.zeros(0, device=DEV)]), norm, 1.0)
+    assert float(norm) == 0
+
+
+def test_plan_refuses():
+    g = torch.zeros(8, device=DEV)
+    for outs in ([torch.zeros(8, dtype=torch.float16, device=DEV)], [torch.zeros(9, device=DEV)], []):
+        with pytest.raises((ValueError, TypeError)):
+            binding.GradPlan([g], outs)
+    with pytest.raises(ValueError):
+        binding.GradPlan([torch.zeros(8, 8, device=DEV).t()])
+    with pytest.raises(binding.RaggedError):
+        binding.ragged_grad_clip(binding.GradPlan([g]), torch.zeros(1, dtype=torch.float64, device=DEV), 0.0)
+
+
+def test_same_bits_every_time_and_in_a_graph():
+    grads = _make([300000, 77, 4096], "bf16", 5)
+    outs = [torch.empty_like(g, dtype=torch.float32) for g in grads]
+    norm = torch.zeros(1, dtype=torch.float64, device=DEV)
+    plan = binding.GradPlan(grads, outs)
+    graph = harness.capture(torch, lambda: binding.ragged_grad_clip(plan, norm, 1.0))
+    for _ in range(3):
+        grads[0].normal_()
+        binding.ragged_grad_clip(plan, norm, 1.0)
+        want = [norm.clone()] + [o.clone() for o in outs]
+        for t in [norm] + outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip([norm] + outs, want))

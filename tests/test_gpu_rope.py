@@ -1,0 +1,132 @@
+"""ragged_rope against complex products in fp64.  Bound: the angle is one turn at most in fp32 (2e-7), its sine and cosine are two
+places off at most (2.4e-7), and the two products and their sum are rounded (3 * 2^-24): 1e-6 of |a| + |b|, and half a step of the output."""
+import pytest
+import torch
+
+from paper_2604_15408_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+_TYPES = {"f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def _reference(x, coords, freqs, index, layout, amplitude, inverse):
+    """(rotated x, |a| + |b| of every element's pair) in fp64 on the CPU."""
+    x, pairs = x.double().cpu(), freqs.numel()
+    rows = x.shape[0]
+    u = torch.arange(rows) if index is None else index[:rows].cpu().long() & 0xFFFFFFFF
+    at = coords.cpu().double()[u % coords.shape[0]]
+    axis = torch.arange(pairs) // (pairs // coords.shape[1])
+    angle = at[:, axis] * freqs.cpu()
+    unit = torch.polar(torch.full_like(angle, amplitude), -angle if inverse else angle)[:, None, :]
+    a, b = (slice(0, pairs), slice(pairs, 2 * pairs)) if layout == "half" else (slice(0, 2 * pairs, 2), slice(1, 2 * pairs, 2))
+    z = torch.complex(x[..., a].contiguous(), x[..., b].contiguous()) * unit
+    y, size = x.clone(), torch.zeros_like(x)
+    y[..., a], y[..., b] = z.real, z.imag
+    size[..., a] = size[..., b] = abs(amplitude) * (x[..., a].abs() + x[..., b].abs())
+    return y, size
+
+
+def _check(got, want, size):
+    eps = torch.finfo(got.dtype).eps / 2
+    err = (got.double().cpu() - want).abs()
+    assert torch.all(err <= eps * want.abs() + 1e-6 * size + 2.0 ** -25), float(err.max())
+
+
+CASES = [  # rows, Hq, Hk, D, pairs, axes, layout
+    (1, 12, 12, 64, 32, 1, "half"), (1, 1, 0, 8, 1, 1, "interleaved"), (37, 3, 3, 64, 32, 2, "half"), (130, 12, 12, 64, 16, 2, "interleaved"),
+    (65, 5, 1, 80, 10, 1, "half"), (65, 5, 1, 80, 10, 2, "interleaved"), (33, 2, 2, 128, 64, 1, "half"), (9, 16, 4, 128, 32, 1, "interleaved"),
+    (7, 1, 1, 512, 256, 2, "half"), (3, 200, 8, 64, 32, 1, "half"), (40, 3, 2, 24, 7, 1, "half"), (5, 3, 0, 64, 30, 3, "interleaved"),
+    (1100, 3, 1, 64, 32, 2, "half"), (9000, 1, 1, 16, 8, 1, "interleaved")]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,hq,hk,d,pairs,axes,layout", CASES)
+def test_rope(rows, hq, hk, d, pairs, axes, layout, dtype):
+    gen = torch.Generator().manual_seed(rows * 7 + d)
+    tdt = _TYPES[dtype]
+    cap = rows + 3
+    fused = torch.randn(cap, hq + hk + 1, d, generator=gen).to(tdt).to(DEV)          # queries, keys, one head that is not theirs
+    q, k = fused[:, :hq], fused[:, hq:hq + hk] if hk else None
+    freqs = binding.rope_frequencies(pairs, 100.0, axes).to(DEV)
+    coords = (torch.randn(29, axes, generator=gen) * 50).to(DEV)
+    index = torch.randint(-5, 1000, (cap,), generator=gen, dtype=torch.int32).to(DEV)
+    valid = torch.tensor([rows], dtype=torch.int32, device=DEV)
+    for inverse, amplitude, ix in ((False, 1.0, index), (True, 1.25, None)):
+        want_q = _reference(q[:rows], coords, freqs, ix, layout, amplitude, inverse)
+        want_k = _reference(k[:rows], coords, freqs, ix, layout, amplitude, inverse) if hk else None
+        # out of place: queries into rows of their own, keys into a wider buffer; rows behind the valid ones as they were
+        q_out = torch.full((cap, hq, d), 9.0, dtype=tdt, device=DEV)
+        wide = torch.full((cap, hk + 2, d), 9.0, dtype=tdt, device=DEV)
+        k_out = wide[:, 1:hk + 1] if hk else None
+        binding.ragged_rope(q, k, q_out, k_out, coords, freqs, ix, layout, amplitude, inverse, valid)
+        _check(q_out[:rows], *want_q)
+        assert torch.all(q_out[rows:] == 9) and torch.all(wide[rows:] == 9)
+        if hk:
+            _check(k_out[:rows], *want_k)
+            assert torch.all(wide[:, 0] == 9) and torch.all(wide[:, hk + 1] == 9)
+        # in place: the same bits
+        both = fused.clone()
+        bq, bk = both[:, :hq], both[:, hq:hq + hk] if hk else None
+        binding.prepare_rope(bq, bk, bq, bk, coords, freqs, ix, layout, amplitude, inverse, valid)()
+        assert torch.equal(bq[:rows], q_out[:rows]) and torch.equal(both[rows:], fused[rows:]) and torch.equal(both[:, hq + hk], fused[:, hq + hk])
+        assert not hk or torch.equal(bk[:rows], k_out[:rows])
+        # queries in place, keys not
+        both = fused.clone()
+        bq = both[:, :hq]
+        if hk:
+            wide.fill_(9.0)
+            binding.ragged_rope(bq, both[:, hq:hq + hk], bq, k_out, coords, freqs, ix, layout, amplitude, inverse, valid)
+            assert torch.equal(bq[:rows], q_out[:rows]) and torch.equal(both[:, hq:], fused[:, hq:])
+            _check(k_out[:rows], *want_k)
+
+
+def test_rope_far_positions():
+    """2^24 - 1 radians: the angle itself needs more than 32 bits."""
+    freqs = binding.rope_frequencies(32).to(DEV)
+    coords = torch.tensor([[2.0 ** 24 - 1], [1234567.0], [99999.5]], device=DEV)
+    q = torch.randn(3, 2, 64, generator=torch.Generator().manual_seed(1)).half().to(DEV)
+    out = torch.empty_like(q)
+    binding.ragged_rope(q, None, out, None, coords, freqs)
+    _check(out, *_reference(q, coords, freqs, None, "half", 1.0, False))
+
+
+def test_rope_inverse_is_the_transpose():
+    """<R x, y> = <x, R' y> in what the two directions compute, and R' R x = m^2 x."""
+    gen = torch.Generator().manual_seed(3)
+    freqs, coords = binding.rope_frequencies(24, 100.0, 2).to(DEV), (torch.randn(50, 2, generator=gen) * 9).to(DEV)
+    x, y = torch.randn(2, 50, 3, 64, generator=gen).half().to(DEV)
+    rx, ry, back = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    binding.ragged_rope(x, None, rx, None, coords, freqs, amplitude=0.5)
+    binding.ragged_rope(y, None, ry, None, coords, freqs, amplitude=0.5, inverse=True)
+    binding.ragged_rope(rx, None, back, None, coords, freqs, amplitude=0.5, inverse=True)
+    dot = lambda p, q: (p.double() * q.double()).sum()
+    # every output is off by half a step (2^-11 of it) and 1e-6: at most that times the sum of the products' sizes
+    size = ((rx.double() * y.double()).abs().sum() + (x.double() * ry.double()).abs().sum()) * 2.0 ** -11 + 1e-5 * x.numel()
+    assert abs(dot(rx, y) - dot(x, ry)) <= size
+    want = x.double() * 0.25
+    want[..., 48:] = x[..., 48:].double()
+    pair = torch.cat((x[..., :24].abs() + x[..., 24:48].abs(),) * 2, dim=-1).double()
+    bound = torch.zeros_like(want)
+    bound[..., :48] = pair * 0.25 * (3 * 2.0 ** -11) + 1e-5
+    assert torch.all((back.double() - want).abs() <= bound)
+
+
+def test_rope_without_rows_and_in_a_graph():
+    from paper_2604_15408_amd import harness
+    freqs = binding.rope_frequencies(32).to(DEV)
+    coords = torch.arange(8, dtype=torch.float32, device=DEV).reshape(8, 1)
+    q = torch.randn(6, 2, 64, device=DEV).half()
+    out = torch.zeros_like(q)
+    for none in (0, -3):
+        binding.ragged_rope(q, None, out, None, coords, freqs, rows_dev=torch.tensor([none], dtype=torch.int32, device=DEV))
+        assert not out.any()
+    graph = harness.capture(torch, lambda: binding.ragged_rope(q, None, out, None, coords, freqs))
+    for _ in range(3):
+        q.normal_()
+        want = torch.empty_like(q)
+        binding.ragged_rope(q, None, want, None, coords, freqs)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
