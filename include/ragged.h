@@ -356,8 +356,8 @@ int ragged_attn_lse(const void* q, const void* k, const void* v, void* o, float*
  *   lse        [T, H]     as it wrote them
  *   dq, dk, dv [T, H, D]  out (dt), grad_tok_stride elements between tokens (for example the slices of a fused [T, 3, H, D] buffer);
  *                         they must not overlap any input.  Rows >= T are left untouched
- *   max_seqlen            an upper bound on every n_i; rows of sequences at positions >= 64 * ceil(max_seqlen / 64) are not computed,
- *                         and their gradients are left untouched
+ *   max_seqlen            an upper bound on every n_i; gradients of rows at positions >= max_seqlen of a longer sequence may be left
+ *                         uncomputed (such a row then stays untouched as a whole)
  *
  * Supported: D = 64, dt = F16 or BF16; every token row on a 16-byte boundary; strides as for ragged_attn_strided (grad_tok_stride as
  * out_tok_stride).  max_seqlen <= 64 * 32767 and half of the work-groups of ragged_attn's limit.  Products on MFMA with fp32 sums;

@@ -107,6 +107,8 @@ class _Ctypes:
     def dev(t, dtype, shape):
         return None
 
+    rows = dev
+
     def __getattr__(self, name):
         return getattr(load(), name)
 
@@ -207,6 +209,9 @@ def ragged_attn(q, k, v, o, cu_seqlens, max_seqlen: int, scale: float, stream=No
 def _token_rows(t: torch.Tensor, name: str, dtype, shape):
     """(pointer, token stride) of a [rows, H, D] view whose tokens are a constant number of elements
     apart and whose [H, D] block is contiguous inside a token (e.g. ``qkv[:, 0]`` of [rows, 3, H, D])."""
+    got = (_marshal or _native()).rows(t, dtype, shape)
+    if got is not None:
+        return got
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
     if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
@@ -460,21 +465,18 @@ def prepare_rope(q, k, q_out, k_out, coords, freqs, index=None, layout: str = "h
                     (q, k, q_out, k_out, coords, freqs, index, rows_dev))
 
 
-def _same_stride(*tensors):
-    """(pointers, token stride) of [rows, H, D] views that share shape, dtype and token stride."""
-    first = tensors[0][0]
-    got = [_token_rows(t, name, _HALF if t is first else first.dtype, first.shape) for t, name in tensors]
-    if len({s for _, s in got}) != 1:
-        raise ValueError(f"{', '.join(n for _, n in tensors)} must share their token stride")
-    return [p for p, _ in got], int(got[0][1])
-
-
 def _attn_lse_args(q, k, v, o, lse, cu_seqlens, max_seqlen, scale, stream):
-    (qp, kp, vp), in_tok = _same_stride((q, "q"), (k, "k"), (v, "v"))
-    op, out_tok = _token_rows(o, "o", q.dtype, q.shape)
-    rows, H, D = q.shape
-    return (qp, kp, vp, op, _dev(lse, "lse", torch.float32, (rows, H)), _dev(cu_seqlens, "cu_seqlens", torch.int32),
-            cu_seqlens.shape[0] - 1, int(max_seqlen), H, D, in_tok, int(out_tok), float(scale), _DTYPE_CODE[q.dtype], _stream(stream))
+    rows = (_marshal or _native()).rows
+    dt, shape = q.dtype, q.shape
+    qp, in_tok = rows(q, _HALF, None) or _token_rows(q, "q", _HALF, None)
+    kp, ks = rows(k, dt, shape) or _token_rows(k, "k", dt, shape)
+    vp, vs = rows(v, dt, shape) or _token_rows(v, "v", dt, shape)
+    op, out_tok = rows(o, dt, shape) or _token_rows(o, "o", dt, shape)
+    if not in_tok == ks == vs:
+        raise ValueError("q, k, v must share their token stride")
+    n, H, D = shape
+    return (qp, kp, vp, op, _dev(lse, "lse", torch.float32, (n, H)), _dev(cu_seqlens, "cu_seqlens", torch.int32),
+            cu_seqlens.numel() - 1, int(max_seqlen), H, D, in_tok, out_tok, float(scale), _DTYPE_CODE[dt], _stream(stream))
 
 
 def ragged_attn_lse(q, k, v, o, lse, cu_seqlens, max_seqlen: int, scale: float, stream=None) -> None:
@@ -488,15 +490,21 @@ def prepare_attn_lse(q, k, v, o, lse, cu_seqlens, max_seqlen: int, scale: float,
 
 
 def _attn_backward_args(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen, scale, stream):
-    (qp, kp, vp), in_tok = _same_stride((q, "q"), (k, "k"), (v, "v"))
-    (op, dop), out_tok = _same_stride((o, "o"), (d_o, "d_o"))
-    (dqp, dkp, dvp), grad_tok = _same_stride((dq, "dq"), (dk, "dk"), (dv, "dv"))
-    for t, name in ((o, "o"), (dq, "dq")):
-        if t.dtype != q.dtype or t.shape != q.shape:
-            raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, expected {tuple(q.shape)} {q.dtype}")
-    rows, H, D = q.shape
-    return (qp, kp, vp, op, dop, _dev(lse, "lse", torch.float32, (rows, H)), dqp, dkp, dvp, _dev(cu_seqlens, "cu_seqlens", torch.int32),
-            cu_seqlens.shape[0] - 1, int(max_seqlen), H, D, in_tok, out_tok, grad_tok, float(scale), _DTYPE_CODE[q.dtype], _stream(stream))
+    rows = (_marshal or _native()).rows
+    dt, shape = q.dtype, q.shape
+    qp, in_tok = rows(q, _HALF, None) or _token_rows(q, "q", _HALF, None)
+    kp, ks = rows(k, dt, shape) or _token_rows(k, "k", dt, shape)
+    vp, vs = rows(v, dt, shape) or _token_rows(v, "v", dt, shape)
+    op, out_tok = rows(o, dt, shape) or _token_rows(o, "o", dt, shape)
+    dop, dos = rows(d_o, dt, shape) or _token_rows(d_o, "d_o", dt, shape)
+    dqp, grad_tok = rows(dq, dt, shape) or _token_rows(dq, "dq", dt, shape)
+    dkp, dks = rows(dk, dt, shape) or _token_rows(dk, "dk", dt, shape)
+    dvp, dvs = rows(dv, dt, shape) or _token_rows(dv, "dv", dt, shape)
+    if not (in_tok == ks == vs and out_tok == dos and grad_tok == dks == dvs):
+        raise ValueError("q, k, v must share their token stride, o and d_o theirs, dq, dk, dv theirs")
+    n, H, D = shape
+    return (qp, kp, vp, op, dop, _dev(lse, "lse", torch.float32, (n, H)), dqp, dkp, dvp, _dev(cu_seqlens, "cu_seqlens", torch.int32),
+            cu_seqlens.numel() - 1, int(max_seqlen), H, D, in_tok, out_tok, grad_tok, float(scale), _DTYPE_CODE[dt], _stream(stream))
 
 
 def ragged_attn_backward(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen: int, scale: float, stream=None) -> None:

@@ -3,20 +3,31 @@
 //     P_ij = exp(c q_i.k_j - L_i),   dP_ij = dO_i.v_j,   dS_ij = P_ij (dP_ij - delta_i),
 //     dV = P^T dO,   dK = c dS^T Q,   dQ = c dS K.
 //
-// One launch, no atomics, no workspace: a work-group owns 64 rows of one (image, head), either as KEYS, whose dK and dV it sums up
-// over all query tiles, or as QUERIES, whose dQ it sums up over all key tiles.  Both form P and dP again from 16-bit rows
-// (seven products instead of the five that a pass over both at once would need), which is what lets every sum have one owner and one order.
+// One launch, no atomics, no workspace.  A sequence of at most 64 rows is one work-group's (whole_sequence: five products, dS turned
+// through LDS).  Of a longer one a work-group owns 128 rows, either as KEYS, whose dK and dV it sums up over all query tiles, or as
+// QUERIES, whose dQ it sums up over all key tiles (own_rows).  Both form P and dP again from 16-bit rows (seven products instead of the
+// five that a pass over both at once would need), which is what lets every sum have one owner and one order.
 //
-// The two roles are one piece of code with the operands exchanged.  A wavefront owns 16 rows ("columns" below: the MFMA's column
-// dimension); tiles of the other side's 64 rows stream through a ring in LDS by direct loads, two operands at a time:
+// The two roles are one piece of code with the operands exchanged.  A wavefront owns 32 rows ("columns" below: the MFMA's column
+// dimension, two blocks of 16); tiles of the other side's 64 rows stream through a ring in LDS by direct loads:
 //     keys:    columns are keys,    tile A = Q, B = dO:   S = Q K^T,   dP = dO V^T;   dV^T += dO^T P,   dK^T += Q^T dS
 //     queries: columns are queries, tile A = K, B = V :   S^T = K Q^T, dP^T = V dO^T;                   dQ^T += K^T dS^T
 // As in the forward pass the first products leave each lane with the scores of ONE column and tile rows 4 (lane/16) + r of every 16,
 // which is the B operand that the second products want, and those read the same row-major tiles transposed: P and dS never leave
-// registers.  LDS layout, swizzle and operand addresses are those of the forward kernel (attn.hip).
+// registers.  LDS layout, swizzle and operand addresses are those of the forward kernel (attn.hip).  Two column blocks share every
+// operand read from LDS: with one the LDS pipe was the bound (32 x 577 tokens, 12 heads, bf16: 258 us with 16 columns a wavefront).
+//
+// delta is the diagonal of dO O^T, two MFMAs for 16 rows.  Past keys the rows of o stream through the ring as a third operand and the
+// statistics of a tile are formed from LDS between two barriers: read by the lanes from memory in front of the loop they cost
+// a work-group of keys a quarter of its time (same case 112 us for the keys alone, 82 without).  - delta is where the sum dP starts.
 //
 // P and dS are rounded to the input type for the second products, as the gradients themselves are in the end: a sum of n terms
 // whose signs are mixed is off by about as much as its own rounding.  Sums are fp32.
+//
+// us now (gradients alone, H = 12): 32 x 577 bf16 144 (82 GFLOP in five products, 115 in the seven of this form: 0.8 PFLOP/s, where a loop of
+// products alone sustains 1.3), 64 x 197 fp16 55 (155 MB of rows: 26 us at the rate of a copy), 32 x about 40 bf16 6.7.
+#include <type_traits>
+
 #include "attn_parts.h"
 #include "common.h"
 #include "mfma_lds.h"
@@ -24,8 +35,16 @@
 namespace ragged {
 namespace {
 
-constexpr int kGroupPairs = 512;        // (image, head) pairs of a dispatch batch, as in the forward pass
-constexpr int kRingBytes = 2 * 2 * kTileBytes;
+constexpr int kOwnBlocks = 2;           // column blocks of a wavefront
+constexpr int kOwnRows = kBlockThreads / kWaveSize * 16 * kOwnBlocks;         // rows of a work-group
+// (image, head) pairs of a dispatch batch: all the work-groups of a batch come before the next one's, those of a pair on one XCD.  As many
+// pairs as have their rows in three quarters of that XCD's 4 MB L2, so that the work-groups of a pair read them there; those of 512, as in
+// the forward pass, would be streamed again and again (64 x 197 tokens: 512 pairs 59 us, 256 61, 128 55; 32 x 577: 512 159, 128 154, 64 144).
+constexpr int kGroupPairs = 512, kGroupPairsMin = 32;
+constexpr int64_t kGroupBytes = 3 << 20;
+constexpr int kSlotBytes = 3 * kTileBytes;      // tiles A and B; keys: the rows of o besides
+constexpr int kLseBytes = kBN * 4;
+constexpr int kLdsBytes = 2 * kSlotBytes + 2 * kLseBytes + 2 * kBN * 4;      // ring, L of a tile's queries, statistics (L log2 e, - delta)
 
 struct BackwardArgs {
     const uint16_t *q, *k, *v, *o, *d_o;
@@ -37,17 +56,28 @@ struct BackwardArgs {
     float scale;
 };
 
-// Sum over d of a[d] b[d], 16 values.
+// dma16 for four bytes a lane: lane i's go to lds_dst + 4 i.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma4(uint32_t lds_dst, uint32_t voff, const void* base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(lds_dst), "v"(voff), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+__device__ __forceinline__ void lds_write8(uint32_t addr, uint2 v) {
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+    *reinterpret_cast<lds_u32x2*>(static_cast<uintptr_t>(addr)) = u32x2{v.x, v.y};
+}
+
+// delta of 16 rows: the diagonal of dO O^T.  A lane brings 16 head-dim elements (16 g ..) of row lane % 16 of both and gets the sum of
+// that row if its group is the row's own (g = row / 4), as exact products added up in fp32.
 template <typename In>
-__device__ __forceinline__ float dot16(const uint4 (&a)[2], const uint4 (&b)[2]) {
-    float sum = 0.f;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const typename In::vec8 x = as_vec8<typename In::vec8>(a[h]), y = as_vec8<typename In::vec8>(b[h]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum = __builtin_fmaf((float)x[e], (float)y[e], sum);
-    }
-    return sum;
+__device__ __forceinline__ float diagonal(const uint4 (&a)[2], const uint4 (&b)[2], int col) {
+    f32x4 d = In::mfma(as_vec8<typename In::vec8>(a[0]), as_vec8<typename In::vec8>(b[0]), f32x4{0.f, 0.f, 0.f, 0.f});
+    d = In::mfma(as_vec8<typename In::vec8>(a[1]), as_vec8<typename In::vec8>(b[1]), d);
+    const float lo = col & 1 ? d[1] : d[0], hi = col & 1 ? d[3] : d[2];
+    return col & 2 ? hi : lo;
 }
 
 // Eight fp32 values of a lane as one operand of a product.
@@ -81,21 +111,25 @@ __device__ __forceinline__ void store_row(BF16, uint16_t* dst, const f32x4 (&acc
     store16(reinterpret_cast<__bf16*>(dst), v);
 }
 
-// One work-group's rows m0 .. m0 + 63 of an image's head as KEYS or as queries.
-template <typename In, bool KEYS>
-__device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* ring, float2 (*stats)[kBN], int s, int n, int h, int m0) {
+// One work-group's rows m0 .. m0 + 64 CB - 1 of an image's head as KEYS or as queries; a wavefront has CB blocks of 16 columns.
+template <typename In, bool KEYS, int CB>
+__device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int s, int n, int h, int m0) {
     typedef typename In::vec8 vec8;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int64_t head = (int64_t)h * kHeadDim;
-    const int own = m0 + wave * 16 + col;                      // this lane's row inside the image
-    const bool active = m0 + wave * 16 < n;
+    const int first = m0 + wave * 16 * CB;                     // the wavefront's rows inside the image
+    const bool active = first < n;
     const float c2 = p.scale * kLog2e;
     // what streams: Q and dO past keys, K and V past queries
     const int tok_a = p.in_tok, tok_b = KEYS ? p.out_tok : p.in_tok;
     const uint16_t* const base_a = (KEYS ? p.q : p.k) + (int64_t)s * tok_a + head;
     const uint16_t* const base_b = (KEYS ? p.d_o : p.v) + (int64_t)s * tok_b + head;
-    const uint32_t ring0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)ring);
+    const uint32_t ring0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)lds);
+    const uint32_t lse0 = ring0 + 2 * kSlotBytes;
+    float* const lse_lds = reinterpret_cast<float*>(lds) + 2 * kSlotBytes / 4;
+    f32x4* const stats = reinterpret_cast<f32x4*>(lse_lds + 2 * kBN);         // [2][kBN / 4]
+    const uint16_t* const base_o = p.o + (int64_t)s * tok_b + head;           // (keys)
     const int tiles = (n + kBN - 1) / kBN;
     const int load_row = 16 * wave + (lane >> 3);
     const uint32_t load_chunk = 16u * ((lane & 7) ^ ((lane >> 4) & 3));
@@ -103,58 +137,46 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* ring, flo
         const int rem = n - t * kBN;
         const int need = rem >= kBN ? kBN : 32 * ((rem + 31) >> 5);       // rows the tile's products touch
         if (16 * wave >= need) return;
-        const uint32_t dst = ring0 + slot * 2 * kTileBytes + wave * 2048;
+        const uint32_t dst = ring0 + slot * kSlotBytes + wave * 2048;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             int rel = load_row + 8 * i;
             rel = rel < rem ? rel : rem - 1;                   // past the end: the last real row again
             dma16(dst + i * 1024, (uint32_t)rel * tok_a * 2u + load_chunk, base_a + (int64_t)t * kBN * tok_a);
             dma16(dst + i * 1024 + kTileBytes, (uint32_t)rel * tok_b * 2u + load_chunk, base_b + (int64_t)t * kBN * tok_b);
+            if (KEYS) dma16(dst + i * 1024 + 2 * kTileBytes, (uint32_t)rel * tok_b * 2u + load_chunk, base_o + (int64_t)t * kBN * tok_b);
         }
+        if (KEYS && wave == 0)
+            dma4(lse0 + slot * kLseBytes, (uint32_t)(lane < rem ? lane : rem - 1) * p.H * 4u, p.lse + ((int64_t)s + t * kBN) * p.H + h);
     };
     issue(0, 0);
 
-    // ---- this lane's column: two operands, 16 head-dim elements (16 g ..) of each (zeros past the end)
-    uint4 own_a[2] = {}, own_b[2] = {};                        // k, v or q, dO
-    float lse2 = 0.f, delta = 0.f;                             // queries: statistics of the column
-    if (own < n) {
-        const int64_t row = (int64_t)s + own;
-        const uint4* a = reinterpret_cast<const uint4*>((KEYS ? p.k : p.q) + row * p.in_tok + head + 16 * g);
-        const uint4* b = reinterpret_cast<const uint4*>(KEYS ? p.v + row * p.in_tok + head + 16 * g : p.d_o + row * p.out_tok + head + 16 * g);
-        own_a[0] = a[0]; own_a[1] = a[1];
-        own_b[0] = b[0]; own_b[1] = b[1];
-        if (!KEYS) {
-            const uint4* o = reinterpret_cast<const uint4*>(p.o + row * p.out_tok + head + 16 * g);
-            const uint4 o_row[2] = {o[0], o[1]};
-            delta = dot16<In>(own_b, o_row);
-            lse2 = p.lse[row * p.H + h] * kLog2e;
+    // ---- this lane's columns: two operands, 16 head-dim elements (16 g ..) of each (zeros past the end)
+    vec8 col_a[CB][2], col_b[CB][2];                           // k, v or q, dO
+    float lse2[CB], minus_delta[CB];                           // queries: statistics of the columns
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        uint4 own_a[2] = {}, own_b[2] = {}, own_o[2] = {};
+        lse2[cb] = minus_delta[cb] = 0.f;
+        const int own = first + 16 * cb + col;
+        if (own < n) {
+            const int64_t row = (int64_t)s + own;
+            const uint4* a = reinterpret_cast<const uint4*>((KEYS ? p.k : p.q) + row * p.in_tok + head + 16 * g);
+            const uint4* b = reinterpret_cast<const uint4*>(KEYS ? p.v + row * p.in_tok + head + 16 * g : p.d_o + row * p.out_tok + head + 16 * g);
+            own_a[0] = a[0]; own_a[1] = a[1];
+            own_b[0] = b[0]; own_b[1] = b[1];
+            if (!KEYS) {
+                const uint4* o = reinterpret_cast<const uint4*>(p.o + row * p.out_tok + head + 16 * g);
+                own_o[0] = o[0]; own_o[1] = o[1];
+                lse2[cb] = p.lse[row * p.H + h] * kLog2e;
+            }
         }
-    }
-    if (!KEYS) delta = quad_sum(delta);
-    const vec8 col_a[2] = {as_vec8<vec8>(own_a[0]), as_vec8<vec8>(own_a[1])};
-    const vec8 col_b[2] = {as_vec8<vec8>(own_b[0]), as_vec8<vec8>(own_b[1])};
-
-    // ---- keys: statistics of the queries of a tile, four threads a row; behind the last one exp2(.. - inf) = 0
-    uint4 st_o[2], st_do[2];
-    float st_lse;
-    auto request_stats = [&](int t) {
-        const int row = t * kBN + (tid >> 2);
-        const int64_t at = (int64_t)s + (row < n ? row : n - 1);
-        const uint4* o = reinterpret_cast<const uint4*>(p.o + at * p.out_tok + head + 16 * (tid & 3));
-        const uint4* d = reinterpret_cast<const uint4*>(p.d_o + at * p.out_tok + head + 16 * (tid & 3));
-        st_o[0] = o[0]; st_o[1] = o[1];
-        st_do[0] = d[0]; st_do[1] = d[1];
-        st_lse = p.lse[at * p.H + h];
-    };
-    auto write_stats = [&](int t) {
-        float d = dot16<In>(st_o, st_do);
-        d += __shfl_xor(d, 1);
-        d += __shfl_xor(d, 2);
-        if ((tid & 3) == 0) stats[t & 1][tid >> 2] = t * kBN + (tid >> 2) < n ? make_float2(st_lse * kLog2e, d) : make_float2(INFINITY, 0.f);
-    };
-    if (KEYS) {
-        request_stats(0);
-        write_stats(0);
+        if (!KEYS) minus_delta[cb] = -__shfl(diagonal<In>(own_b, own_o, col), 16 * (col >> 2) + col);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            col_a[cb][ks] = as_vec8<vec8>(own_a[ks]);
+            col_b[cb][ks] = as_vec8<vec8>(own_b[ks]);
+        }
     }
 
     // LDS addresses of this lane inside a tile, as in the forward kernel
@@ -162,90 +184,255 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* ring, flo
     const int tr_row = 4 * g + (col >> 2);
     const uint32_t tr_rel = tr_row * 128 + 16 * ((2 * (col & 3)) ^ ((tr_row >> 1) & 3));
 
-    f32x4 acc_a[4], acc_b[4];                                  // dK^T or dQ^T; dV^T
+    // The columns count as used here: a load that the compiler still believes in flight inside the loop makes it wait there for all
+    // memory traffic, the next tile's among it.
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt) acc_a[dt] = acc_b[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int cb = 0; cb < CB; ++cb) {
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) asm volatile("" : "+v"(col_a[cb][ks]), "+v"(col_b[cb][ks]));
+        asm volatile("" : "+v"(lse2[cb]), "+v"(minus_delta[cb]));
+    }
+    f32x4 acc_a[CB][4], acc_b[CB][4];                          // dK^T or dQ^T; dV^T
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) acc_a[cb][dt] = acc_b[cb][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+    // keys: the statistics of a tile's queries, 16 of them by each wavefront; behind the last query exp2(.. - inf) = 0
+    auto write_stats = [&](int t, int slot) {
+        const uint32_t rb = ring0 + slot * kSlotBytes + kTileBytes + row_rel + wave * 16 * 128, ro = rb + kTileBytes;
+        const uint4 d[2] = {lds_read16(rb), lds_read16(rb ^ 16u)}, o[2] = {lds_read16(ro), lds_read16(ro ^ 16u)};
+        const float delta = diagonal<In>(d, o, col);
+        if (g == col >> 2) {
+            const bool there = t * kBN + 16 * wave + col < n;
+            reinterpret_cast<float*>(stats)[16 * wave + col] = there ? lse_lds[slot * kBN + 16 * wave + col] * kLog2e : INFINITY;
+            reinterpret_cast<float*>(stats)[kBN + 16 * wave + col] = there ? -delta : 0.f;
+        }
+    };
+
+    // 32 rows of a tile: MASK where some of them may lie behind the last key
+    auto block = [&](uint32_t tile, int bb, int rem, auto mask) {
+        constexpr bool MASK = decltype(mask)::value;
+        f32x4 pr[CB][2], ds[CB][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int kt = 2 * bb + u;
+            const uint32_t ra = tile + row_rel + kt * 16 * 128, rb = ra + kTileBytes;
+            const vec8 a0 = as_vec8<vec8>(lds_read16(ra)), a1 = as_vec8<vec8>(lds_read16(ra ^ 16u));
+            const vec8 b0 = as_vec8<vec8>(lds_read16(rb)), b1 = as_vec8<vec8>(lds_read16(rb ^ 16u));
+            f32x4 row_lse, row_delta;
+            if (KEYS) {
+                row_lse = stats[4 * kt + g];
+                row_delta = stats[kBN / 4 + 4 * kt + g];
+            }
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                const f32x4 from = KEYS ? row_delta : f32x4{minus_delta[cb], minus_delta[cb], minus_delta[cb], minus_delta[cb]};
+                f32x4 sc = In::mfma(a0, col_a[cb][0], f32x4{0.f, 0.f, 0.f, 0.f});
+                f32x4 dp = In::mfma(b0, col_b[cb][0], from);   // dP - delta: delta is where the sum starts
+                sc = In::mfma(a1, col_a[cb][1], sc);
+                dp = In::mfma(b1, col_b[cb][1], dp);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], c2, KEYS ? -row_lse[r] : -lse2[cb]));
+                    if (MASK && !KEYS) e = 16 * kt + 4 * g + r < rem ? e : 0.f;
+                    pr[cb][u][r] = e;
+                    ds[cb][u][r] = e * dp[r];
+                }
+            }
+        }
+        vec8 ds_op[CB], p_op[CB];
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            ds_op[cb] = operand(In{}, ds[cb][0], ds[cb][1]);
+            if (KEYS) p_op[cb] = operand(In{}, pr[cb][0], pr[cb][1]);
+        }
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+            const uint32_t a = tile + (((dt & 2) ? tr_rel ^ 16u : tr_rel) + 8 * (dt & 1) + bb * 32 * 128);
+            const uint2 lo = __builtin_bit_cast(uint2, lds_read_tr(a)), hi = __builtin_bit_cast(uint2, lds_read_tr(a + 16 * 128));
+            const vec8 at = as_vec8<vec8>(make_uint4(lo.x, lo.y, hi.x, hi.y));
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) acc_a[cb][dt] = In::mfma(at, ds_op[cb], acc_a[cb][dt]);
+            if (KEYS) {
+                const uint2 lo2 = __builtin_bit_cast(uint2, lds_read_tr(a + kTileBytes)),
+                            hi2 = __builtin_bit_cast(uint2, lds_read_tr(a + kTileBytes + 16 * 128));
+                const vec8 bt = as_vec8<vec8>(make_uint4(lo2.x, lo2.y, hi2.x, hi2.y));
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) acc_b[cb][dt] = In::mfma(bt, p_op[cb], acc_b[cb][dt]);
+            }
+        }
+    };
     for (int t = 0; t < tiles; ++t) {
         const int slot = t & 1;
         wait_vm<0>();
         __syncthreads();                                       // tile t is there; everyone is past the reads of tile t - 1
-        if (t + 1 < tiles) {
-            issue(t + 1, slot ^ 1);
-            if (KEYS) request_stats(t + 1);
+        if (t + 1 < tiles) issue(t + 1, slot ^ 1);
+        if (KEYS) {
+            if (t * kBN + 16 * wave < n + 16) write_stats(t, slot);
+            __syncthreads();
         }
         if (active) {
-            const uint32_t tile = ring0 + slot * 2 * kTileBytes;
+            const uint32_t tile = ring0 + slot * kSlotBytes;
             const int rem = n - t * kBN;
-            const int blocks = rem >= 32 + 1 ? 2 : 1;          // of 32 rows
-#pragma unroll
-            for (int bb = 0; bb < 2; ++bb) {
-                if (bb >= blocks) break;
-                f32x4 pr[2], ds[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int kt = 2 * bb + u;
-                    const uint32_t ra = tile + row_rel + kt * 16 * 128;
-                    f32x4 sc = In::mfma(as_vec8<vec8>(lds_read16(ra)), col_a[0], f32x4{0.f, 0.f, 0.f, 0.f});
-                    sc = In::mfma(as_vec8<vec8>(lds_read16((ra ^ 16u))), col_a[1], sc);
-                    const uint32_t rb = ra + kTileBytes;
-                    f32x4 dp = In::mfma(as_vec8<vec8>(lds_read16(rb)), col_b[0], f32x4{0.f, 0.f, 0.f, 0.f});
-                    dp = In::mfma(as_vec8<vec8>(lds_read16((rb ^ 16u))), col_b[1], dp);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int row = 16 * kt + 4 * g + r;
-                        float l2 = lse2, dl = delta;
-                        if (KEYS) {
-                            const float2 st = stats[slot][row];
-                            l2 = st.x;
-                            dl = st.y;
-                        }
-                        float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], c2, -l2));
-                        if (!KEYS) e = row < rem ? e : 0.f;
-                        pr[u][r] = e;
-                        ds[u][r] = e * (dp[r] - dl);
-                    }
-                }
-                const vec8 ds_op = operand(In{}, ds[0], ds[1]);
-                vec8 p_op;
-                if (KEYS) p_op = operand(In{}, pr[0], pr[1]);
-#pragma unroll
-                for (int dt = 0; dt < 4; ++dt) {
-                    const uint32_t a = tile + (((dt & 2) ? tr_rel ^ 16u : tr_rel) + 8 * (dt & 1) + bb * 32 * 128);
-                    const uint2 lo = __builtin_bit_cast(uint2, lds_read_tr(a)), hi = __builtin_bit_cast(uint2, lds_read_tr(a + 16 * 128));
-                    acc_a[dt] = In::mfma(as_vec8<vec8>(make_uint4(lo.x, lo.y, hi.x, hi.y)), ds_op, acc_a[dt]);
-                    if (KEYS) {
-                        const uint2 lo2 = __builtin_bit_cast(uint2, lds_read_tr(a + kTileBytes)),
-                                    hi2 = __builtin_bit_cast(uint2, lds_read_tr(a + kTileBytes + 16 * 128));
-                        acc_b[dt] = In::mfma(as_vec8<vec8>(make_uint4(lo2.x, lo2.y, hi2.x, hi2.y)), p_op, acc_b[dt]);
-                    }
-                }
+            if (KEYS || rem >= kBN) {
+                const int blocks = rem > 32 ? 2 : 1;
+#pragma nounroll
+                for (int bb = 0; bb < blocks; ++bb) block(tile, bb, rem, std::false_type{});
+            } else {
+#pragma nounroll
+                for (int bb = 0; 32 * bb < rem; ++bb) block(tile, bb, rem, std::true_type{});
             }
         }
-        if (KEYS && t + 1 < tiles) write_stats(t + 1);
     }
-    // this lane owns elements 16 g .. 16 g + 15 of its row
-    if (own < n) {
-        const int64_t at = ((int64_t)s + own) * p.grad_tok + head + 16 * g;
-        store_row(In{}, (KEYS ? p.dk : p.dq) + at, acc_a, p.scale);
-        if (KEYS) store_row(In{}, p.dv + at, acc_b, 1.0f);
+    // this lane owns elements 16 g .. 16 g + 15 of its rows
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        const int own = first + 16 * cb + col;
+        if (own < n) {
+            const int64_t at = ((int64_t)s + own) * p.grad_tok + head + 16 * g;
+            store_row(In{}, (KEYS ? p.dk : p.dq) + at, acc_a[cb], p.scale);
+            if (KEYS) store_row(In{}, p.dv + at, acc_b[cb], 1.0f);
+        }
     }
 }
 
+// A whole sequence of at most 64 rows: P and dS are formed once, dS goes through LDS to the products that want it by queries.
 template <typename In>
-__global__ __launch_bounds__(kBlockThreads)
+__device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds, int s, int n, int h) {
+    typedef typename In::vec8 vec8;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, g = lane >> 4;
+    const int64_t head = (int64_t)h * kHeadDim;
+    const float c2 = p.scale * kLog2e;
+    const uint32_t q0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)lds);
+    const uint32_t do0 = q0 + kTileBytes, o0 = q0 + 2 * kTileBytes, k0 = q0 + 3 * kTileBytes, ds0 = q0 + 4 * kTileBytes;
+    const uint32_t lse0 = q0 + 2 * kSlotBytes;
+    float* const lse_lds = reinterpret_cast<float*>(lds) + 2 * kSlotBytes / 4;
+    f32x4* const stats = reinterpret_cast<f32x4*>(lse_lds + 2 * kBN);
+    const int blocks = (n + 31) >> 5;                          // of 32 rows: what the products touch
+    if (wave < 2 * blocks) {
+        const uint32_t chunk = 16u * ((lane & 7) ^ ((lane >> 4) & 3));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            int rel = 16 * wave + 8 * i + (lane >> 3);
+            rel = rel < n ? rel : n - 1;                       // past the end: the last real row again
+            const uint32_t in = (uint32_t)rel * p.in_tok * 2u + chunk, out = (uint32_t)rel * p.out_tok * 2u + chunk;
+            const uint32_t at = wave * 2048 + i * 1024;
+            dma16(q0 + at, in, p.q + (int64_t)s * p.in_tok + head);
+            dma16(do0 + at, out, p.d_o + (int64_t)s * p.out_tok + head);
+            dma16(o0 + at, out, p.o + (int64_t)s * p.out_tok + head);
+            dma16(k0 + at, in, p.k + (int64_t)s * p.in_tok + head);
+        }
+        if (wave == 0) dma4(lse0, (uint32_t)(lane < n ? lane : n - 1) * p.H * 4u, p.lse + (int64_t)s * p.H + h);
+    }
+    // this lane's key: k and v, head-dim elements 16 g .. (zeros past the end)
+    const int own = 16 * wave + col;
+    uint4 own_k[2] = {}, own_v[2] = {};
+    if (own < n) {
+        const int64_t at = ((int64_t)s + own) * p.in_tok + head + 16 * g;
+        const uint4 *k = reinterpret_cast<const uint4*>(p.k + at), *v = reinterpret_cast<const uint4*>(p.v + at);
+        own_k[0] = k[0]; own_k[1] = k[1];
+        own_v[0] = v[0]; own_v[1] = v[1];
+    }
+    const vec8 kf[2] = {as_vec8<vec8>(own_k[0]), as_vec8<vec8>(own_k[1])}, vf[2] = {as_vec8<vec8>(own_v[0]), as_vec8<vec8>(own_v[1])};
+    const uint32_t row_rel = col * 128 + 16 * ((2 * g) ^ ((col >> 1) & 3));
+    const int tr_row = 4 * g + (col >> 2);
+    const uint32_t tr_rel = tr_row * 128 + 16 * ((2 * (col & 3)) ^ ((tr_row >> 1) & 3));
+    wait_vm<0>();
+    __syncthreads();
+    const bool active = wave < 2 * blocks;                     // (a wavefront past the last key still fills its part of dS with zeros)
+    if (active) {
+        const uint32_t rb = do0 + row_rel + wave * 2048, ro = o0 + row_rel + wave * 2048;
+        const uint4 d[2] = {lds_read16(rb), lds_read16(rb ^ 16u)}, o[2] = {lds_read16(ro), lds_read16(ro ^ 16u)};
+        const float delta = diagonal<In>(d, o, col);
+        if (g == col >> 2) {
+            reinterpret_cast<float*>(stats)[own] = own < n ? lse_lds[own] * kLog2e : INFINITY;
+            reinterpret_cast<float*>(stats)[kBN + own] = own < n ? -delta : 0.f;
+        }
+    }
+    __syncthreads();
+    f32x4 acc_k[4], acc_v[4];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) acc_k[dt] = acc_v[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto transposed = [&](uint32_t tile, int dt, int bb) {
+        const uint32_t a = tile + (((dt & 2) ? tr_rel ^ 16u : tr_rel) + 8 * (dt & 1) + bb * 32 * 128);
+        const uint2 lo = __builtin_bit_cast(uint2, lds_read_tr(a)), hi = __builtin_bit_cast(uint2, lds_read_tr(a + 16 * 128));
+        return as_vec8<vec8>(make_uint4(lo.x, lo.y, hi.x, hi.y));
+    };
+    if (active) {
+#pragma unroll
+        for (int bb = 0; bb < 2; ++bb) {
+            if (bb >= blocks) break;
+            f32x4 pr[2], ds[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int kt = 2 * bb + u;
+                const uint32_t ra = q0 + row_rel + kt * 2048, rb = do0 + row_rel + kt * 2048;
+                const f32x4 row_lse = stats[4 * kt + g];
+                pr[u] = In::mfma(as_vec8<vec8>(lds_read16(ra)), kf[0], f32x4{0.f, 0.f, 0.f, 0.f});
+                ds[u] = In::mfma(as_vec8<vec8>(lds_read16(rb)), vf[0], stats[kBN / 4 + 4 * kt + g]);
+                pr[u] = In::mfma(as_vec8<vec8>(lds_read16(ra ^ 16u)), kf[1], pr[u]);
+                ds[u] = In::mfma(as_vec8<vec8>(lds_read16(rb ^ 16u)), vf[1], ds[u]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    pr[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(pr[u][r], c2, -row_lse[r]));
+                    ds[u][r] = own < n ? pr[u][r] * ds[u][r] : 0.f;
+                }
+            }
+            const vec8 p_op = operand(In{}, pr[0], pr[1]), ds_op = operand(In{}, ds[0], ds[1]);
+            // dS by keys: row own, queries 16 kt + 4 g .. + 3 in the same swizzled order as the other tiles
+            const uint4 w = __builtin_bit_cast(uint4, ds_op);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t at = ds0 + own * 128 + 16 * ((2 * (2 * bb + u) + (g >> 1)) ^ ((own >> 1) & 3)) + 8 * (g & 1);
+                lds_write8(at, u ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y));
+            }
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) {
+                acc_k[dt] = In::mfma(transposed(q0, dt, bb), ds_op, acc_k[dt]);
+                acc_v[dt] = In::mfma(transposed(do0, dt, bb), p_op, acc_v[dt]);
+            }
+        }
+        if (own < n) {
+            const int64_t at = ((int64_t)s + own) * p.grad_tok + head + 16 * g;
+            store_row(In{}, p.dk + at, acc_k, p.scale);
+            store_row(In{}, p.dv + at, acc_v, 1.0f);
+        }
+    }
+    __syncthreads();
+    // dQ^T += K^T dS^T: in the transposed read this wavefront's columns are the queries 16 (col / 4) + 4 wave + col % 4
+    const int query = 16 * (col >> 2) + 4 * wave + (col & 3);
+    f32x4 acc_q[4];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) acc_q[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int bb = 0; bb < 2; ++bb) {
+        if (bb >= blocks) break;
+        const vec8 ds_op = transposed(ds0, wave, bb);
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) acc_q[dt] = In::mfma(transposed(k0, dt, bb), ds_op, acc_q[dt]);
+    }
+    if (query < n) store_row(In{}, p.dq + ((int64_t)s + query) * p.grad_tok + head + 16 * g, acc_q, p.scale);
+}
+
+template <typename In>
+__global__ __launch_bounds__(kBlockThreads, 3)             // three work-groups on a CU: 168 registers, 49 KB of LDS
 void attn_backward_kernel(BackwardArgs p) {
-    __shared__ __attribute__((aligned(1024))) uint4 ring[kRingBytes / 16];     // [slot][A | B]
-    __shared__ float2 stats[2][kBN];                           // of a tile's queries: L log2 e, delta
+    __shared__ __attribute__((aligned(1024))) uint4 lds[kLdsBytes / 16];
     const int pair = blockIdx.z * p.group + blockIdx.x;
     if (pair >= p.pairs) return;
     uint32_t img, h;
     divmod((uint32_t)pair, (uint32_t)p.H, p.h_magic, img, h);
     const int s = p.cu_seqlens[img], n = __builtin_amdgcn_readfirstlane(p.cu_seqlens[img + 1] - s);
-    const int m0 = (blockIdx.y >> 1) * kBN;
+    const int m0 = (blockIdx.y >> 1) * kOwnRows;
     if (m0 >= n) return;
-    if (blockIdx.y & 1) own_rows<In, false>(p, ring, stats, s, n, (int)h, m0);
-    else own_rows<In, true>(p, ring, stats, s, n, (int)h, m0);
+    if (n <= kBN) {
+        if (blockIdx.y == 0) whole_sequence<In>(p, lds, s, n, (int)h);
+        return;
+    }
+    if (blockIdx.y & 1) own_rows<In, false, kOwnBlocks>(p, lds, s, n, (int)h, m0);
+    else own_rows<In, true, kOwnBlocks>(p, lds, s, n, (int)h, m0);
 }
 
 }  // namespace
@@ -253,9 +440,13 @@ void attn_backward_kernel(BackwardArgs p) {
 hipError_t launch_attn_backward(const void* q, const void* k, const void* v, const void* o, const void* d_o, const float* lse, void* dq, void* dk,
                                 void* dv, const int32_t* cu_seqlens, int B, int max_seqlen, int H, int64_t in_tok, int64_t out_tok,
                                 int64_t grad_tok, float scale, ragged_dtype dt, hipStream_t stream) {
-    const int pairs = B * H, tiles = (max_seqlen + kBN - 1) / kBN;
+    const int pairs = B * H, tiles = (max_seqlen + kOwnRows - 1) / kOwnRows;
+    int group = kGroupPairs;
+    while (group > kGroupPairsMin && (int64_t)group / kXcds * max_seqlen * (5 * kHeadDim * 2) > kGroupBytes) group /= 2;
+    while ((pairs + group - 1) / group > kMaxGridYZ) group *= 2;              // (ends: the C ABI layer has checked it for 512)
     const int pairs8 = (pairs + kXcds - 1) / kXcds * kXcds;
-    const int group = pairs8 < kGroupPairs ? pairs8 : kGroupPairs, batches = (pairs + group - 1) / group;
+    if (group > pairs8) group = pairs8;
+    const int batches = (pairs + group - 1) / group;
     const BackwardArgs p{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v),
                          static_cast<const uint16_t*>(o), static_cast<const uint16_t*>(d_o), static_cast<uint16_t*>(dq),
                          static_cast<uint16_t*>(dk), static_cast<uint16_t*>(dv), lse, cu_seqlens, H, pairs, group, (int)in_tok, (int)out_tok,

@@ -59,6 +59,30 @@ PyObject* dev(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
 }
 
+// rows(tensor, dtype, shape) -> (address, elements between tokens) of a [rows, H, D] GPU view of that type and shape whose [H, D] block is
+// contiguous inside a token, or None.  With fewer than two tokens the distance is at least one row.
+PyObject* rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 3) {
+        PyErr_SetString(PyExc_TypeError, "rows takes a tensor, a dtype and a shape");
+        return nullptr;
+    }
+    if (!THPVariable_CheckExact(args[0])) Py_RETURN_NONE;
+    try {
+        const at::Tensor& t = THPVariable_Unpack(args[0]);
+        if (!t.is_cuda() || t.dim() != 3 || t.stride(2) != 1 || t.stride(1) != t.size(2)) Py_RETURN_NONE;
+        if (args[1] != Py_None && !dtype_is(args[1], t.scalar_type())) Py_RETURN_NONE;
+        if (args[2] != Py_None && !shape_is(args[2], t.sizes())) Py_RETURN_NONE;
+        const int64_t row = t.size(1) * t.size(2), stride = t.size(0) > 1 || t.stride(0) > row ? t.stride(0) : row;
+        PyObject* const out = PyTuple_New(2);
+        if (!out) return nullptr;
+        PyTuple_SET_ITEM(out, 0, PyLong_FromVoidPtr(t.data_ptr()));
+        PyTuple_SET_ITEM(out, 1, PyLong_FromLongLong(stride));
+        return out;
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
 template <typename T>
 bool convert(PyObject* o, T& out) {
     if constexpr (std::is_pointer_v<T>) {
@@ -97,6 +121,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) { return invoke(
 #define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<&name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     {"dev", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&dev)), METH_FASTCALL, nullptr},
+    {"rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&rows)), METH_FASTCALL, nullptr},
     ENTRY(ragged_pack), ENTRY(ragged_attn), ENTRY(ragged_attn_strided), ENTRY(ragged_attn_checked), ENTRY(ragged_attn_padded),
     ENTRY(ragged_unpack), ENTRY(ragged_repack), ENTRY(ragged_cls_extract), ENTRY(ragged_pack_attn_unpack), ENTRY(ragged_linear),
     ENTRY(ragged_layernorm), ENTRY(ragged_token_scores_l2), ENTRY(ragged_keep_topk), ENTRY(ragged_noop),
