@@ -13,11 +13,17 @@
 namespace ragged {
 namespace {
 
-// kChunksHalf, kChunksInterleaved: 16 bytes at a time, where the pairs of a head fill whole chunks; kSinglePairs: any other number of pairs.
-enum { kChunksHalf = 0, kChunksInterleaved = 1, kSinglePairs = 2 };
+// W values at a time: as many as the pairs of a head (half) or its rotated part (interleaved) can be shared out in, up to 16 bytes.
+enum { kHalf = 0, kInterleaved = 1 };
+template <int W> struct Words { typedef uint32_t type __attribute__((ext_vector_type(W / 2))); };
+template <> struct Words<2> { typedef uint32_t type; };
+template <> struct Words<1> { typedef uint16_t type; };
 constexpr int kRopeAhead = 4;                                  // units a thread requests before the angles are there
 constexpr int kRopeRows = 16;                                  // rows of a work-group at most
 constexpr int kRopeAngles = 2048;                              // angles of a work-group at most (16 KB of LDS)
+// Output beyond half of the last-level cache goes past it: 168 MB alone 51 us instead of 75 over and over, 72 instead of 77 from HBM, and
+// with a kernel that reads it next 104 instead of 102.  Below, the next kernel finds it there (57 MB: 27 us and 38 with its reader either way).
+constexpr int64_t kRopeBypass = 128 << 20;                     // bytes
 constexpr int kRopeFill = 512;                                 // work-groups below which rows are not gathered into fewer
 
 struct RopeArgs {
@@ -30,7 +36,7 @@ struct RopeArgs {
     const int32_t* index;                                      // [rows] or null
     const double* freqs;                                       // [pairs]
     int64_t q_stride, k_stride, q_out_stride, k_out_stride;    // elements from row to row
-    int rows_cap, rows_per, Hq, D, pairs, interleaved;
+    int rows_cap, rows_per, Hq, D, pairs;
     int unit_heads, per_head;                                  // heads of a row (queries, then keys), units of a head
     int rotated;                                               // units of a head that rotate; the others copy
     int axes, n_coords;
@@ -46,11 +52,34 @@ __device__ __forceinline__ void turn(float& a, float& b, float2 cs) {
     a = u;
 }
 
-template <typename In, int FORM>
+// Values of a row as fp32 and back, rounded once.
+template <typename In, int W>
+__device__ __forceinline__ void widen(const typename Words<W>::type& w, float (&v)[W]) {
+    if constexpr (W == 1) {
+        float two[2];
+        LinearLine<2>{{(uint32_t)w}}.unpack(In{}, two);
+        v[0] = two[0];
+    } else {
+        const LinearLine<W> l = __builtin_bit_cast(LinearLine<W>, w);
+        l.unpack(In{}, v);
+    }
+}
+template <typename In, int W>
+__device__ __forceinline__ typename Words<W>::type narrow(const float (&v)[W]) {
+    if constexpr (W == 1) {
+        const float two[2] = {v[0], 0.f};
+        return (uint16_t)LinearLine<2>::pack(In{}, two).w[0];
+    } else {
+        return __builtin_bit_cast(typename Words<W>::type, LinearLine<W>::pack(In{}, v));
+    }
+}
+
+template <typename In, int LAYOUT, int W, bool BYPASS = false>
 __global__ __launch_bounds__(kBlockThreads)
 void rope_kernel(RopeArgs p) {
-    typedef LinearLine<8> Chunk;
-    typedef LinearLine<2> Word;
+    typedef typename Words<W>::type Line;
+    constexpr int CW = LAYOUT == kHalf && W < 8 ? 2 * W : W;   // values at a time of what is copied
+    typedef typename Words<CW>::type CopyLine;
     __shared__ float2 angle[kRopeAngles];                      // [row][pair]: m cos t, m sin t
     int rows = p.rows_cap;
     if (p.rows_dev) { const int r = *p.rows_dev; rows = r < rows ? r : rows; }
@@ -74,63 +103,53 @@ void rope_kernel(RopeArgs p) {
         at.dst = (key ? p.k_out + row * p.k_out_stride : p.q_out + row * p.q_out_stride) + off;
         return at;
     };
-    struct Values { Chunk a, b; };                             // (the forms that take less use the first words of it)
+    // interleaved: what rotates and what is copied lie in one row of equal lines; half: a unit has two lines, a copied one a line of its own width
+    struct Values { Line a, b; };
+    static_assert(sizeof(CopyLine) <= sizeof(Values), "a copied unit's values are kept in place of a pair's");
     auto load = [&](const Place& at) {
-        Values v{};
+        Values v;
         const uint32_t j = at.piece;
-        if (FORM == kSinglePairs) {
-            if (j >= (uint32_t)p.rotated) v.a.w[0] = *reinterpret_cast<const uint32_t*>(at.src + 2 * j);
-            else if (p.interleaved) v.a.w[0] = *reinterpret_cast<const uint32_t*>(at.src + 2 * j);
-            else v.a.w[0] = at.src[j] | (uint32_t)at.src[j + p.pairs] << 16;
-        } else if (FORM == kChunksInterleaved) {
-            v.a = *reinterpret_cast<const Chunk*>(at.src + 8 * j);
+        if (LAYOUT == kInterleaved) {
+            v.a = *reinterpret_cast<const Line*>(at.src + W * j);
         } else if (j < (uint32_t)p.rotated) {
-            v.a = *reinterpret_cast<const Chunk*>(at.src + 8 * j);
-            v.b = *reinterpret_cast<const Chunk*>(at.src + 8 * j + p.pairs);
+            v.a = *reinterpret_cast<const Line*>(at.src + W * j);
+            v.b = *reinterpret_cast<const Line*>(at.src + W * j + p.pairs);
         } else {
-            v.a = *reinterpret_cast<const Chunk*>(at.src + 8 * j + p.pairs);
+            const CopyLine c = *reinterpret_cast<const CopyLine*>(at.src + 2 * p.pairs + CW * (j - p.rotated));
+            __builtin_memcpy(&v, &c, sizeof(c));
         }
         return v;
     };
-    auto finish = [&](const Place& at, Values v) {
+    auto put = [&](uint16_t* dst, auto line) {
+        typedef decltype(line) T;
+        if constexpr (BYPASS) __builtin_nontemporal_store(line, reinterpret_cast<T*>(dst));
+        else *reinterpret_cast<T*>(dst) = line;
+    };
+    auto finish = [&](const Place& at, const Values& v) {
         const uint32_t j = at.piece;
-        const bool copy = j >= (uint32_t)p.rotated;
-        const float2* cs = angle + at.row * p.pairs;
-        if (FORM == kSinglePairs) {
-            if (!copy) {
-                Word w{{v.a.w[0]}};
-                float x[2];
-                w.unpack(In{}, x);
-                turn(x[0], x[1], cs[j]);
-                w = Word::pack(In{}, x);
-                v.a.w[0] = w.w[0];
-                if (!p.interleaved) {
-                    at.dst[j] = (uint16_t)w.w[0];
-                    at.dst[j + p.pairs] = (uint16_t)(w.w[0] >> 16);
-                    return;
-                }
+        if (j >= (uint32_t)p.rotated) {
+            if (LAYOUT == kInterleaved) {
+                put(at.dst + W * j, v.a);
+            } else {
+                CopyLine c;
+                __builtin_memcpy(&c, &v, sizeof(c));
+                put(at.dst + 2 * p.pairs + CW * (j - p.rotated), c);
             }
-            *reinterpret_cast<uint32_t*>(at.dst + 2 * j) = v.a.w[0];
-        } else if (FORM == kChunksInterleaved) {
-            if (!copy) {
-                float x[8];
-                v.a.unpack(In{}, x);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) turn(x[2 * e], x[2 * e + 1], cs[4 * j + e]);
-                v.a = Chunk::pack(In{}, x);
-            }
-            *reinterpret_cast<Chunk*>(at.dst + 8 * j) = v.a;
-        } else if (copy) {
-            *reinterpret_cast<Chunk*>(at.dst + 8 * j + p.pairs) = v.a;
-        } else {
-            float x[8], y[8];
-            v.a.unpack(In{}, x);
-            v.b.unpack(In{}, y);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) turn(x[e], y[e], cs[8 * j + e]);
-            *reinterpret_cast<Chunk*>(at.dst + 8 * j) = Chunk::pack(In{}, x);
-            *reinterpret_cast<Chunk*>(at.dst + 8 * j + p.pairs) = Chunk::pack(In{}, y);
+            return;
         }
+        const float2* cs = angle + at.row * p.pairs;
+        float x[W], y[W];
+        widen<In, W>(v.a, x);
+        if constexpr (LAYOUT == kHalf) {
+            widen<In, W>(v.b, y);
+#pragma unroll
+            for (int e = 0; e < W; ++e) turn(x[e], y[e], cs[W * j + e]);
+            put(at.dst + W * j + p.pairs, narrow<In, W>(y));
+        } else {
+#pragma unroll
+            for (int e = 0; e < W / 2; ++e) turn(x[2 * e], x[2 * e + 1], cs[W / 2 * j + e]);
+        }
+        put(at.dst + W * j, narrow<In, W>(x));
     };
 
     Values ahead[kRopeAhead];
@@ -187,36 +206,43 @@ hipError_t launch_rope(const void* q, const void* k, void* q_out, void* k_out, i
     p.Hq = Hq;
     p.D = D;
     p.pairs = pairs;
-    p.interleaved = interleaved;
     p.axes = axes;
     p.n_coords = n_coords;
     p.amplitude = amplitude;
     p.inverse = inverse;
-    // 16 bytes at a time where the rotated part is whole chunks
-    const int form = interleaved ? (pairs % 4 == 0 ? kChunksInterleaved : kSinglePairs) : (pairs % 8 == 0 ? kChunksHalf : kSinglePairs);
-    p.rotated = form == kChunksHalf ? pairs / 8 : form == kChunksInterleaved ? pairs / 4 : pairs;
-    const int copied = form == kSinglePairs ? (D - 2 * pairs) / 2 : (D - 2 * pairs) / 8;
+    const int shared = interleaved ? 2 * pairs : pairs;
+    const int w = shared % 8 == 0 ? 8 : shared % 4 == 0 ? 4 : shared % 2 == 0 ? 2 : 1;
+    const int cw = interleaved || w == 8 ? w : 2 * w;
+    p.rotated = shared / w;
     const bool in_place = q_out == q && k_out == k;            // what is not rotated is there already
-    p.per_head = p.rotated + (in_place ? 0 : copied);
+    p.per_head = p.rotated + (in_place ? 0 : (D - 2 * pairs) / cw);
     p.unit_heads = Hq + (k ? Hk : 0);
     const int row_units = p.unit_heads * p.per_head;
-    // as many rows as a thread's units ahead allow, fewer where there would be too few work-groups
-    int per = kRopeAhead * kBlockThreads / row_units;
-    per = per < rows_cap / kRopeFill ? per : rows_cap / kRopeFill;
-    per = per < kRopeAngles / pairs ? per : kRopeAngles / pairs;
-    per = per < kRopeRows ? per : kRopeRows;
-    p.rows_per = per < 1 ? 1 : per;
+    // As few rows as keep 15 of 16 threads busy (or those that keep most), but not so many that there would be too few work-groups.
+    // 18 464 rows of 96 units from HBM: 2, 5 and 10 rows 27.0, 27.4 and 29.6 us; 32 774 of 320: 1, 2 and 3 rows 93, 97 and 77.
+    int most = rows_cap / kRopeFill < kRopeAngles / pairs ? rows_cap / kRopeFill : kRopeAngles / pairs;
+    most = most < kRopeRows ? most : kRopeRows;
+    p.rows_per = 1;
+    double best = 0.0;
+    for (int per = 1; per <= most && (per == 1 || per * row_units <= kRopeAhead * kBlockThreads); ++per) {
+        const int units = per * row_units, slots = (units + kBlockThreads - 1) / kBlockThreads * kBlockThreads;
+        const double busy = (double)units / slots;
+        if (busy > best) { best = busy; p.rows_per = per; }
+        if (busy >= 0.9375) break;
+    }
     p.row_magic = div_magic((uint32_t)row_units);
     p.head_magic = div_magic((uint32_t)p.per_head);
     p.pair_magic = div_magic((uint32_t)pairs);
     p.axis_magic = div_magic((uint32_t)(pairs / axes));
     p.coord_magic = div_magic((uint32_t)n_coords);
+    const bool bypass = (int64_t)rows_cap * p.unit_heads * D * 2 > kRopeBypass;
     const dim3 grid((unsigned)(((int64_t)rows_cap + p.rows_per - 1) / p.rows_per));
     auto typed = [&](auto in) {
         typedef decltype(in) In;
-        return form == kChunksHalf ? launch_kernel(rope_kernel<In, kChunksHalf>, grid, dim3(kBlockThreads), stream, p)
-             : form == kChunksInterleaved ? launch_kernel(rope_kernel<In, kChunksInterleaved>, grid, dim3(kBlockThreads), stream, p)
-                                          : launch_kernel(rope_kernel<In, kSinglePairs>, grid, dim3(kBlockThreads), stream, p);
+        auto launch = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(kBlockThreads), stream, p); };
+        if (w == 8 && bypass) return launch(interleaved ? rope_kernel<In, kInterleaved, 8, true> : rope_kernel<In, kHalf, 8, true>);
+        if (interleaved) return launch(w == 8 ? rope_kernel<In, kInterleaved, 8> : w == 4 ? rope_kernel<In, kInterleaved, 4> : rope_kernel<In, kInterleaved, 2>);
+        return launch(w == 8 ? rope_kernel<In, kHalf, 8> : w == 4 ? rope_kernel<In, kHalf, 4> : w == 2 ? rope_kernel<In, kHalf, 2> : rope_kernel<In, kHalf, 1>);
     };
     return dt == RAGGED_F16 ? typed(F16{}) : typed(BF16{});
 }

@@ -37,6 +37,7 @@ CASES = [  # rows, Hq, Hk, D, pairs, axes, layout
     (1, 12, 12, 64, 32, 1, "half"), (1, 1, 0, 8, 1, 1, "interleaved"), (37, 3, 3, 64, 32, 2, "half"), (130, 12, 12, 64, 16, 2, "interleaved"),
     (65, 5, 1, 80, 10, 1, "half"), (65, 5, 1, 80, 10, 2, "interleaved"), (33, 2, 2, 128, 64, 1, "half"), (9, 16, 4, 128, 32, 1, "interleaved"),
     (7, 1, 1, 512, 256, 2, "half"), (3, 200, 8, 64, 32, 1, "half"), (40, 3, 2, 24, 7, 1, "half"), (5, 3, 0, 64, 30, 3, "interleaved"),
+    (50, 3, 3, 64, 12, 1, "half"), (21, 2, 1, 80, 20, 2, "half"), (600, 16, 0, 40, 20, 1, "half"),
     (1100, 3, 1, 64, 32, 2, "half"), (9000, 1, 1, 16, 8, 1, "interleaved")]
 
 
@@ -130,3 +131,18 @@ def test_rope_without_rows_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rope_outputs_larger_than_the_caches(layout):
+    """More than 128 MB of output: the same bits as in pieces."""
+    rows, hq, hk, d = 70001, 12, 3, 64
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    q, k = (torch.randn(rows, h, d, generator=gen, device=DEV).half() for h in (hq, hk))
+    freqs, coords = binding.rope_frequencies(16).to(DEV), torch.arange(rows, dtype=torch.float32, device=DEV).reshape(-1, 1)
+    out, want = (torch.empty_like(q), torch.empty_like(k)), (torch.empty_like(q), torch.empty_like(k))
+    binding.ragged_rope(q, k, *out, coords, freqs, layout=layout)
+    for lo in range(0, rows, 30000):
+        s = slice(lo, lo + 30000)
+        binding.ragged_rope(q[s], k[s], want[0][s], want[1][s], coords[s], freqs, layout=layout)
+    assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
