@@ -4,7 +4,7 @@
 //     dV = P^T dO,   dK = c dS^T Q,   dQ = c dS K.
 //
 // One launch, no atomics, no workspace.  A sequence of at most 64 rows is one work-group's (whole_sequence: five products, dS turned
-// through LDS).  Of a longer one a work-group owns 128 rows, either as KEYS, whose dK and dV it sums up over all query tiles, or as
+// through LDS).  Of a longer one a work-group owns 128 rows (64 in small launches), either as KEYS, whose dK and dV it sums up over all query tiles, or as
 // QUERIES, whose dQ it sums up over all key tiles (own_rows).  Both form P and dP again from 16-bit rows (seven products instead of the
 // five that a pass over both at once would need), which is what lets every sum have one owner and one order.
 //
@@ -35,8 +35,10 @@
 namespace ragged {
 namespace {
 
-constexpr int kOwnBlocks = 2;           // column blocks of a wavefront
-constexpr int kOwnRows = kBlockThreads / kWaveSize * 16 * kOwnBlocks;         // rows of a work-group
+// Launches of at most this many work-groups of 128 rows take work-groups of 64 (CB = 1): CUs would be idle.  us with 64 / 128 rows: 2 x 197
+// tokens, 3 heads 5.7 / 7.6, 4 x 197, 12 heads (192 groups) 8.8 / 10.7, 8 x 197 (384) 12.5 / 13.2, 16 x 128 (384) 10.2 / 10.5; beyond, 32 x 197 at
+// keep 0.5 (1536) 15.2 / 14.4, 64 x 197 63 / 55, 32 x 577 184 / 144.
+constexpr int kSmallGroups = 512;
 // (image, head) pairs of a dispatch batch: all the work-groups of a batch come before the next one's, those of a pair on one XCD.  As many
 // pairs as have their rows in three quarters of that XCD's 4 MB L2, so that the work-groups of a pair read them there; those of 512, as in
 // the forward pass, would be streamed again and again (64 x 197 tokens: 512 pairs 59 us, 256 61, 128 55; 32 x 577: 512 159, 128 154, 64 144).
@@ -416,7 +418,7 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
     if (query < n) store_row(In{}, p.dq + ((int64_t)s + query) * p.grad_tok + head + 16 * g, acc_q, p.scale);
 }
 
-template <typename In>
+template <typename In, int CB>
 __global__ __launch_bounds__(kBlockThreads, 3)             // three work-groups on a CU: 168 registers, 49 KB of LDS
 void attn_backward_kernel(BackwardArgs p) {
     __shared__ __attribute__((aligned(1024))) uint4 lds[kLdsBytes / 16];
@@ -425,14 +427,14 @@ void attn_backward_kernel(BackwardArgs p) {
     uint32_t img, h;
     divmod((uint32_t)pair, (uint32_t)p.H, p.h_magic, img, h);
     const int s = p.cu_seqlens[img], n = __builtin_amdgcn_readfirstlane(p.cu_seqlens[img + 1] - s);
-    const int m0 = (blockIdx.y >> 1) * kOwnRows;
+    const int m0 = (blockIdx.y >> 1) * 64 * CB;
     if (m0 >= n) return;
     if (n <= kBN) {
         if (blockIdx.y == 0) whole_sequence<In>(p, lds, s, n, (int)h);
         return;
     }
-    if (blockIdx.y & 1) own_rows<In, false, kOwnBlocks>(p, lds, s, n, (int)h, m0);
-    else own_rows<In, true, kOwnBlocks>(p, lds, s, n, (int)h, m0);
+    if (blockIdx.y & 1) own_rows<In, false, CB>(p, lds, s, n, (int)h, m0);
+    else own_rows<In, true, CB>(p, lds, s, n, (int)h, m0);
 }
 
 }  // namespace
@@ -440,7 +442,8 @@ void attn_backward_kernel(BackwardArgs p) {
 hipError_t launch_attn_backward(const void* q, const void* k, const void* v, const void* o, const void* d_o, const float* lse, void* dq, void* dk,
                                 void* dv, const int32_t* cu_seqlens, int B, int max_seqlen, int H, int64_t in_tok, int64_t out_tok,
                                 int64_t grad_tok, float scale, ragged_dtype dt, hipStream_t stream) {
-    const int pairs = B * H, tiles = (max_seqlen + kOwnRows - 1) / kOwnRows;
+    const int pairs = B * H;
+    const int own = (int64_t)pairs * 2 * ((max_seqlen + 127) / 128) <= kSmallGroups ? 64 : 128, tiles = (max_seqlen + own - 1) / own;
     int group = kGroupPairs;
     while (group > kGroupPairsMin && (int64_t)group / kXcds * max_seqlen * (5 * kHeadDim * 2) > kGroupBytes) group /= 2;
     while ((pairs + group - 1) / group > kMaxGridYZ) group *= 2;              // (ends: the C ABI layer has checked it for 512)
@@ -452,8 +455,11 @@ hipError_t launch_attn_backward(const void* q, const void* k, const void* v, con
                          static_cast<uint16_t*>(dk), static_cast<uint16_t*>(dv), lse, cu_seqlens, H, pairs, group, (int)in_tok, (int)out_tok,
                          (int)grad_tok, div_magic((uint32_t)H), scale};
     const dim3 grid(group, 2 * tiles, batches);
-    return dt == RAGGED_F16 ? launch_kernel(attn_backward_kernel<F16>, grid, dim3(kBlockThreads), stream, p)
-                            : launch_kernel(attn_backward_kernel<BF16>, grid, dim3(kBlockThreads), stream, p);
+    auto typed = [&](auto in) {
+        typedef decltype(in) In;
+        return launch_kernel(own == 64 ? attn_backward_kernel<In, 1> : attn_backward_kernel<In, 2>, grid, dim3(kBlockThreads), stream, p);
+    };
+    return dt == RAGGED_F16 ? typed(F16{}) : typed(BF16{});
 }
 
 }  // namespace ragged

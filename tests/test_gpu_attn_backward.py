@@ -181,3 +181,19 @@ def test_a_bound_that_is_too_small_leaves_rows():
     binding.ragged_attn_backward(q, k, v, o, do, lse, dq, dk, dv, cu, 70, 0.125)
     for a, b in zip((dq, dk, dv), want):
         assert torch.equal(a[:128], b[:128]) and torch.all(a[128:] == 7)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_small_and_large_launches_agree(dtype):
+    """The same sequences in a launch of their own (64 rows a work-group) and among many (128): the same bits."""
+    lengths = [197, 65, 130, 33]
+    rows, q, k, v, do, cu = _inputs(lengths, 3, dtype, 19, extra=0)
+    few = _run(q, k, v, do, cu, 197, 0.125)
+    many = 70
+    more = torch.from_numpy(np.concatenate([[0], np.cumsum(lengths * many)]).astype(np.int32)).to(DEV)
+    lot = [t.repeat(many, 1, 1) for t in (q, k, v, do)]
+    o, lse = few[0].repeat(many, 1, 1), few[1].repeat(many, 1)
+    grads = [torch.zeros_like(lot[0]) for _ in range(3)]
+    binding.ragged_attn_backward(*lot[:3], o, lot[3], lse, *grads, more, 197, 0.125)
+    for a, b in zip(few[2:], grads):
+        assert torch.equal(a.repeat(many, 1, 1), b)

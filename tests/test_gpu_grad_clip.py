@@ -130,3 +130,12 @@ def test_same_bits_every_time_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip([norm] + outs, want))
+
+
+def test_outputs_larger_than_the_caches():
+    """More values than are left in the caches: 40 million, the last tensor odd."""
+    grads = _make([20000000, 19999999], "bf16", 6, 0.01)
+    outs = [torch.empty_like(g, dtype=torch.float32) for g in grads]
+    norm = torch.zeros(1, dtype=torch.float64, device=DEV)
+    binding.ragged_grad_clip(binding.GradPlan(grads, outs), norm, 1.0, scale=0.5)
+    _check(grads, outs, 0.5, 1.0, norm)
