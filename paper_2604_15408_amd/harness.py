@@ -558,6 +558,98 @@ class ProgressiveBlocks:
         return total
 
 
+class AttentionTraining:
+    """A training step through the attention halves of `depth` pre-norm blocks with rotary positions, on packed rows:
+        h = LN(x); q, k, v = h Wqkv^T + b; q, k = rope(q, k); a = attention; x = x + a Wo^T + b
+    forward, back from a given gradient of the last x, and the gradients of all parameters clipped by their norm into one
+    fp32 buffer.  A patch's position is its place in the square grid of the unpruned image, found through gather_idx; the class token is
+    at the origin.  Every launch of this library takes the row count from the device; rows beyond it stay zero in every buffer, so the
+    weights' gradients are plain library products over the whole buffers.  The input gradient of a linear layer is ragged_linear with
+    the transposed weight."""
+
+    def __init__(self, w, depth: int = 4, max_norm: float = 1.0):
+        import math
+
+        import torch
+        from paper_2604_15408_amd import binding
+        from paper_2604_15408_amd import workloads as wl
+        self.torch, self.b, self.w, self.depth, self.max_norm = torch, binding, w, depth, max_norm
+        dev = "cuda:0"
+        B, N, C, H, D = w.B, w.N, w.C, w.H, w.D
+        cap = self.cap = B * N
+        tdt = torch.float16 if w.dtype == "f16" else torch.bfloat16
+        z = lambda *shape, dt=tdt: torch.zeros(*shape, dtype=dt, device=dev)
+        self.x_in, self.keep = w.features().to(dev), w.keep.to(dev)
+        self.cu, self.gidx = z(B + 1, dt=torch.int32), z(cap, dt=torch.int32)
+        self.rows = self.cu[B:]
+        self.params = []
+        for i in range(depth):
+            p = {k: v.to(dev) for k, v in wl.block_weights(C, 64, w.dtype, 2000 + i).items() if k in ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o")}
+            p["w_qkv_t"], p["w_o_t"] = p["w_qkv"].t().contiguous(), p["w_o"].t().contiguous()
+            self.params.append(p)
+        side = max(1, math.isqrt(N - 1)) if N > 1 else 1
+        patch = torch.arange(N) - 1
+        self.coords = torch.stack((patch // side, patch % side), dim=1).clamp(min=0).float()
+        self.coords[0] = 0
+        self.coords = self.coords.to(dev)
+        self.freqs = binding.rope_frequencies(D // 2, 100.0, axes=2).to(dev)
+        # kept for the way back: the input of every block, its normalised rows, rotated q and k with v, attention and its row statistics
+        self.x = [z(cap, C) for _ in range(depth + 1)]
+        self.h, self.qkv = [z(cap, C) for _ in range(depth)], [z(cap, 3, H, D) for _ in range(depth)]
+        self.a, self.lse = [z(cap, H, D) for _ in range(depth)], [z(cap, H, dt=torch.float32) for _ in range(depth)]
+        self.d_x, self.d_a, self.d_qkv, self.d_h = z(cap, C), z(cap, H, D), z(cap, 3, H, D), z(cap, C)
+        self.workspace = z(binding.layernorm_backward_workspace(cap, C), dt=torch.uint8)
+        self.grads = []
+        for _ in range(depth):
+            self.grads.append({"ln1_g": z(C, dt=torch.float32), "ln1_b": z(C, dt=torch.float32), "w_qkv": z(3 * C, C), "b_qkv": z(1, 3 * C),
+                               "w_o": z(C, C), "b_o": z(1, C)})
+        flat = [g for block in self.grads for g in block.values()]
+        self.clipped = z(sum(g.numel() for g in flat), dt=torch.float32)
+        outs = [o.view_as(g) for o, g in zip(self.clipped.split([g.numel() for g in flat]), flat)]
+        self.plan, self.norm = binding.GradPlan(flat, outs), z(1, dt=torch.float64)
+        self.ones = torch.ones(1, cap, dtype=tdt, device=dev)
+        torch.cuda.synchronize()
+
+    def forward(self):
+        b, w, rows = self.b, self.w, self.rows
+        C = w.C
+        b.ragged_pack(self.x_in, self.keep, self.x[0], self.cu, self.gidx)
+        for i, p in enumerate(self.params):
+            q, k, v = self.qkv[i].unbind(1)
+            b.ragged_layernorm(self.x[i], p["ln1_g"], p["ln1_b"], self.h[i], rows, LN_EPS)
+            b.ragged_linear(self.h[i], p["w_qkv"], p["b_qkv"], None, self.qkv[i].view(self.cap, 3 * C), rows)
+            b.ragged_rope(q, k, q, k, self.coords, self.freqs, index=self.gidx, rows_dev=rows)
+            b.ragged_attn_lse(q, k, v, self.a[i], self.lse[i], self.cu, w.N, w.scale)
+            b.ragged_linear(self.a[i].view(self.cap, C), p["w_o"], p["b_o"], self.x[i], self.x[i + 1], rows)
+
+    def backward(self, d_last):
+        """d_last [cap, C]: the gradient of the last x, zero beyond the valid rows."""
+        b, w, rows, torch = self.b, self.w, self.rows, self.torch
+        C = w.C
+        self.d_x.copy_(d_last)
+        for i in reversed(range(self.depth)):
+            p, g = self.params[i], self.grads[i]
+            q, k, v = self.qkv[i].unbind(1)
+            dq, dk, dv = self.d_qkv.unbind(1)
+            d_a, d_qkv = self.d_a.view(self.cap, C), self.d_qkv.view(self.cap, 3 * C)
+            torch.mm(self.d_x.t(), self.a[i].view(self.cap, C), out=g["w_o"])
+            torch.mm(self.ones, self.d_x, out=g["b_o"])
+            b.ragged_linear(self.d_x, p["w_o_t"], None, None, d_a, rows)
+            b.ragged_attn_backward(q, k, v, self.a[i], self.d_a, self.lse[i], dq, dk, dv, self.cu, w.N, w.scale)
+            b.ragged_rope(dq, dk, dq, dk, self.coords, self.freqs, index=self.gidx, inverse=True, rows_dev=rows)
+            torch.mm(d_qkv.t(), self.h[i], out=g["w_qkv"])
+            torch.mm(self.ones, d_qkv, out=g["b_qkv"])
+            b.ragged_linear(d_qkv, p["w_qkv_t"], None, None, self.d_h, rows)
+            b.ragged_layernorm_backward(self.x[i], p["ln1_g"], self.d_h, self.d_x, g["ln1_g"], g["ln1_b"], self.workspace,
+                                        residual_grad=self.d_x, rows_dev=rows, eps=LN_EPS)
+
+    def run(self):
+        """One step for the loss sum(x^2) / 2 over the last block's rows, whose gradient is x itself."""
+        self.forward()
+        self.backward(self.x[self.depth])
+        self.b.ragged_grad_clip(self.plan, self.norm, self.max_norm)
+
+
 class Ceilings:
     """What this GPU actually reaches on the two resources the rooflines are drawn against: a streaming read
     and a streaming copy of 1 GiB (HBM) and a register-resident fp16 MFMA loop (matrix cores).  The kernels

@@ -9,7 +9,8 @@ flops a padded dense attention has to spend, with no mask cost added); the 384x3
 the 12-layer progressive-pruning loop captured in ONE HIP graph, both through the padded tensor every
 layer (36 kernels) and staying packed (17 kernels); eight packed encoder blocks ("late blocks": LayerNorm,
 QKV projection, ragged attention, output projection, MLP with GELU, residuals) with synthetic weights,
-next to the same blocks over all B*N rows, and with three independent batches in flight on three streams.  Kernel times are HIP-event times
+next to the same blocks over all B*N rows, and with three independent batches in flight on three streams; a training step through the
+attention halves of packed blocks with rotary positions, its gradients clipped by their norm.  Kernel times are HIP-event times
 of a graph holding 20 back-to-back copies of the kernel (divided by 20), so they include the
 in-graph kernel-to-kernel gap that an empty kernel shows separately.
 """
@@ -21,7 +22,7 @@ import os
 import sys
 
 from . import workloads as wl
-from .harness import (REPLICAS, PackedBlocks, PaddedPath, Path, Pipeline, ProgressiveBlocks, StayPackedPipeline, capture, pick_streams,
+from .harness import (REPLICAS, AttentionTraining, PackedBlocks, PaddedPath, Path, Pipeline, ProgressiveBlocks, StayPackedPipeline, capture, pick_streams,
                       event_time_us, wall_steps)
 
 
@@ -224,6 +225,29 @@ def progressive_case(torch, B: int, label: str):
             "images_per_s_3_in_flight": B / per_batch}
 
 
+def training_case(torch, w, label: str, depth: int = 4):
+    """Forward, backward and clipping of `depth` attention halves, step by step (the library products for the weights are not captured),
+    and the kernels of this library that only training has, alone."""
+    tr = AttentionTraining(w, depth)
+    tr.run()
+    torch.cuda.synchronize()
+    step_us = event_time_us(torch, tr.run, iters=20)[0]
+    b = tr.b
+    q, k, v = tr.qkv[0].unbind(1)
+    dq, dk, dv = tr.d_qkv.unbind(1)
+    calls = {"rope": lambda: b.ragged_rope(dq, dk, dq, dk, tr.coords, tr.freqs, index=tr.gidx, rows_dev=tr.rows),
+             "attn_lse": lambda: b.ragged_attn_lse(q, k, v, tr.a[0], tr.lse[0], tr.cu, w.N, w.scale),
+             "attn_backward": lambda: b.ragged_attn_backward(q, k, v, tr.a[0], tr.d_a, tr.lse[0], dq, dk, dv, tr.cu, w.N, w.scale),
+             "layernorm_backward": lambda: b.ragged_layernorm_backward(tr.x[0], tr.params[0]["ln1_g"], tr.d_h, tr.d_x, tr.grads[0]["ln1_g"],
+                                                                       tr.grads[0]["ln1_b"], tr.workspace, residual_grad=tr.d_x, rows_dev=tr.rows),
+             "grad_clip": lambda: b.ragged_grad_clip(tr.plan, tr.norm, tr.max_norm)}
+    us = {}
+    for name, call in calls.items():
+        us[name] = event_time_us(torch, capture(torch, call, REPLICAS).replay, iters=20)[0] / REPLICAS
+    return {"case": label, "workload": w.name, "B": w.B, "N": w.N, "T": w.T, "dtype": w.dtype, "depth": depth, "step_us": step_us,
+            "kernel_us": us, "parameters": tr.clipped.numel(), "images_per_s": w.B / (step_us * 1e-6)}
+
+
 def prune_once_case(torch, B: int, H: int, label: str):
     """The paper's Section 4.3 schedule on a 12-block encoder of DeiT width H*64 with synthetic weights: four
     blocks on all tokens, one pruning stage (top-k l2 score) in front of block 4, eight blocks on the packed
@@ -362,6 +386,9 @@ def main():
             emit(prune_once_case(torch, 32, H, f"prune_once_deit_{name}_bs32"))
         emit(prune_once_case(torch, 8, 12, "prune_once_deit_base_bs8"))
         emit(prune_once_case(torch, 128, 12, "prune_once_deit_base_bs128"))
+    if want("training"):
+        emit(training_case(torch, wl.deit_b_pruned(0.2, 32, "bf16", 1001), "training_keep0.2_bs32"))
+        emit(training_case(torch, wl.deit_b_pruned(1.0, 64, "bf16", 1006), "training_dense_bs64"))
     if want("progressive"):
         emit(progressive_case(torch, 32, "progressive_12_blocks_bs32"))
         emit(progressive_case(torch, 8, "progressive_12_blocks_bs8"))
