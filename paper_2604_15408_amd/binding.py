@@ -8,6 +8,7 @@ been built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import warnings
 from pathlib import Path
 
@@ -108,6 +109,10 @@ class _Ctypes:
         return None
 
     rows = dev
+
+    @staticmethod
+    def here(device, *tensors):
+        return all(t is None or t.device.index == device for t in tensors)
 
     def __getattr__(self, name):
         return getattr(load(), name)
@@ -411,6 +416,15 @@ def ragged_unpack(src, keep, cu_seqlens, gather_idx, out, fill_mode: int, stream
 # ---- training on packed rows ------------------------------------------------------------------------------------------------
 
 _HALF = (torch.float16, torch.bfloat16)
+
+
+def _here(*tensors) -> None:
+    """The kernels run on the current device: every tensor has to be there."""
+    device = _raw_device() if _raw_device is not None else torch.cuda.current_device()
+    if not (_marshal or _native()).here(device, *tensors):
+        raise ValueError(f"a tensor is not on the current device (cuda:{device})")
+
+
 _ROPE_LAYOUT = {"half": 0, "interleaved": 1}
 _ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
 
@@ -443,6 +457,7 @@ def _rope_args(q, k, q_out, k_out, coords, freqs, index, layout, amplitude, inve
             raise ValueError(f"k has shape {tuple(k.shape)}, expected [{rows}, heads, {d}]")
     if coords.dim() != 2:
         raise ValueError("coords must be [n, axes]")
+    _here(q, k, q_out, k_out, coords, freqs, index, rows_dev)
     return (qp, kp, qop, kop, rows, _rows_dev(rows_dev), hq, hk, d, qs, ks, qos, kos, _dev(coords, "coords", torch.float32),
             coords.shape[0], coords.shape[1], None if index is None else _dev(index, "index", torch.int32, (rows,)),
             _dev(freqs, "freqs", torch.float64), freqs.numel(), _ROPE_LAYOUT[layout], float(amplitude), int(bool(inverse)),
@@ -474,6 +489,7 @@ def _attn_lse_args(q, k, v, o, lse, cu_seqlens, max_seqlen, scale, stream):
     op, out_tok = rows(o, dt, shape) or _token_rows(o, "o", dt, shape)
     if not in_tok == ks == vs:
         raise ValueError("q, k, v must share their token stride")
+    _here(q, k, v, o, lse, cu_seqlens)
     n, H, D = shape
     return (qp, kp, vp, op, _dev(lse, "lse", torch.float32, (n, H)), _dev(cu_seqlens, "cu_seqlens", torch.int32),
             cu_seqlens.numel() - 1, int(max_seqlen), H, D, in_tok, out_tok, float(scale), _DTYPE_CODE[dt], _stream(stream))
@@ -502,6 +518,7 @@ def _attn_backward_args(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen
     dvp, dvs = rows(dv, dt, shape) or _token_rows(dv, "dv", dt, shape)
     if not (in_tok == ks == vs and out_tok == dos and grad_tok == dks == dvs):
         raise ValueError("q, k, v must share their token stride, o and d_o theirs, dq, dk, dv theirs")
+    _here(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens)
     n, H, D = shape
     return (qp, kp, vp, op, dop, _dev(lse, "lse", torch.float32, (n, H)), dqp, dkp, dvp, _dev(cu_seqlens, "cu_seqlens", torch.int32),
             cu_seqlens.numel() - 1, int(max_seqlen), H, D, in_tok, out_tok, grad_tok, float(scale), _DTYPE_CODE[dt], _stream(stream))
@@ -520,6 +537,7 @@ def prepare_attn_backward(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seql
                     (q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens))
 
 
+@functools.lru_cache(maxsize=256)                              # (a function of two sizes)
 def layernorm_backward_workspace(rows: int, C: int) -> int:
     """Bytes of workspace that ragged_layernorm_backward needs for up to `rows` rows of width C."""
     need = int(load().ragged_layernorm_backward_workspace(int(rows), int(C)))
@@ -533,10 +551,12 @@ def _layernorm_backward_args(x, gamma, dy, dx, dgamma, dbeta, workspace, residua
     need = layernorm_backward_workspace(rows, C)
     if workspace.numel() * workspace.element_size() < need:
         raise ValueError(f"workspace has {workspace.numel() * workspace.element_size()} bytes, {need} are needed")
-    return (_dev(x, "x", _HALF), _dev(gamma, "gamma", x.dtype, (C,)), _dev(dy, "dy", x.dtype, (rows, C)),
+    args = (_dev(x, "x", _HALF), _dev(gamma, "gamma", x.dtype, (C,)), _dev(dy, "dy", x.dtype, (rows, C)),
             None if residual_grad is None else _dev(residual_grad, "residual_grad", x.dtype, (rows, C)), _dev(dx, "dx", x.dtype, (rows, C)),
             _dev(dgamma, "dgamma", torch.float32, (C,)), _dev(dbeta, "dbeta", torch.float32, (C,)), _dev(workspace, "workspace"), rows,
             _rows_dev(rows_dev), C, float(eps), _DTYPE_CODE[x.dtype], _stream(stream))
+    _here(x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad, rows_dev)
+    return args
 
 
 def ragged_layernorm_backward(x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad=None, rows_dev=None, eps: float = 1e-6,
@@ -594,6 +614,7 @@ class GradPlan:
 
 
 def _grad_clip_args(plan, norm, max_norm, scale, stream):
+    _here(plan.table, norm)
     return (plan.table.data_ptr(), plan.chunks, float(scale), float(max_norm), plan.workspace.data_ptr(),
             _dev(norm, "norm", torch.float64, (1,)), _stream(stream))
 

@@ -19,7 +19,7 @@ template <int W> struct Words { typedef uint32_t type __attribute__((ext_vector_
 template <> struct Words<2> { typedef uint32_t type; };
 template <> struct Words<1> { typedef uint16_t type; };
 constexpr int kRopeAhead = 4;                                  // units a thread requests before the angles are there
-constexpr int kRopeRows = 16;                                  // rows of a work-group at most
+constexpr int kRopeRows = 64;                                  // rows of a work-group at most
 constexpr int kRopeAngles = 2048;                              // angles of a work-group at most (16 KB of LDS)
 // Output beyond half of the last-level cache goes past it: 168 MB alone 51 us instead of 75 over and over, 72 instead of 77 from HBM, and
 // with a kernel that reads it next 104 instead of 102.  Below, the next kernel finds it there (57 MB: 27 us and 38 with its reader either way).
@@ -83,8 +83,9 @@ void rope_kernel(RopeArgs p) {
     __shared__ float2 angle[kRopeAngles];                      // [row][pair]: m cos t, m sin t
     int rows = p.rows_cap;
     if (p.rows_dev) { const int r = *p.rows_dev; rows = r < rows ? r : rows; }
-    const int row0 = blockIdx.x * p.rows_per;
-    if (row0 >= rows) return;
+    const int64_t group_row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * p.rows_per;
+    if (group_row0 >= rows) return;
+    const int row0 = (int)group_row0;
     const int n = rows - row0 < p.rows_per ? rows - row0 : p.rows_per;
     const uint32_t units = (uint32_t)n * p.unit_heads * p.per_head;
     const uint32_t row_units = (uint32_t)p.unit_heads * p.per_head;
@@ -236,7 +237,9 @@ hipError_t launch_rope(const void* q, const void* k, void* q_out, void* k_out, i
     p.axis_magic = div_magic((uint32_t)(pairs / axes));
     p.coord_magic = div_magic((uint32_t)n_coords);
     const bool bypass = (int64_t)rows_cap * p.unit_heads * D * 2 > kRopeBypass;
-    const dim3 grid((unsigned)(((int64_t)rows_cap + p.rows_per - 1) / p.rows_per));
+    const int64_t groups = ((int64_t)rows_cap + p.rows_per - 1) / p.rows_per;
+    constexpr int64_t kGridX = 1 << 20;                        // (threads along a dimension of the grid have to fit 32 bits)
+    const dim3 grid((unsigned)(groups < kGridX ? groups : kGridX), (unsigned)((groups + kGridX - 1) / kGridX));
     auto typed = [&](auto in) {
         typedef decltype(in) In;
         auto launch = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(kBlockThreads), stream, p); };

@@ -83,6 +83,17 @@ PyObject* rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
 }
 
+// here(device, tensor or None, ...) -> whether all tensors are on that device
+PyObject* here(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    const long device = n > 0 ? PyLong_AsLong(args[0]) : -1;
+    if (PyErr_Occurred()) return nullptr;
+    for (Py_ssize_t i = 1; i < n; ++i) {
+        if (args[i] == Py_None) continue;
+        if (!THPVariable_Check(args[i]) || THPVariable_Unpack(args[i]).device().index() != device) Py_RETURN_FALSE;
+    }
+    Py_RETURN_TRUE;
+}
+
 template <typename T>
 bool convert(PyObject* o, T& out) {
     if constexpr (std::is_pointer_v<T>) {
@@ -122,6 +133,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) { return invoke(
 PyMethodDef methods[] = {
     {"dev", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&dev)), METH_FASTCALL, nullptr},
     {"rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&rows)), METH_FASTCALL, nullptr},
+    {"here", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&here)), METH_FASTCALL, nullptr},
     ENTRY(ragged_pack), ENTRY(ragged_attn), ENTRY(ragged_attn_strided), ENTRY(ragged_attn_checked), ENTRY(ragged_attn_padded),
     ENTRY(ragged_unpack), ENTRY(ragged_repack), ENTRY(ragged_cls_extract), ENTRY(ragged_pack_attn_unpack), ENTRY(ragged_linear),
     ENTRY(ragged_layernorm), ENTRY(ragged_token_scores_l2), ENTRY(ragged_keep_topk), ENTRY(ragged_noop),

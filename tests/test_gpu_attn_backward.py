@@ -197,3 +197,22 @@ def test_small_and_large_launches_agree(dtype):
     binding.ragged_attn_backward(*lot[:3], o, lot[3], lse, *grads, more, 197, 0.125)
     for a, b in zip(few[2:], grads):
         assert torch.equal(a.repeat(many, 1, 1), b)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_lse_leaves_the_output_as_it_is(dtype):
+    """Launches in phases and with key-split wavefronts: o is ragged_attn_strided's, bit for bit, and lse that of the row sums."""
+    for lengths, H in (([577, 301] * 16, 12), ([300, 1, 64, 65, 128], 3)):
+        rows, q, k, v, do, cu = _inputs(lengths, H, dtype, 20, extra=0)
+        o, want = torch.full_like(q, 7.0), torch.full_like(q, 9.0)
+        lse = torch.full((rows, H), 7.0, device=DEV)
+        binding.prepare_attn_lse(q, k, v, o, lse, cu, max(lengths), -0.125)()
+        binding.ragged_attn_strided(q, k, v, want, cu, max(lengths), -0.125)
+        assert torch.equal(o, want)
+        for i in (0, len(lengths) - 1):
+            lo, hi = int(cu[i]), int(cu[i + 1])
+            a, b = (t[lo:hi].cpu().double().transpose(0, 1) for t in (q, k))
+            s = -0.125 * (a @ b.transpose(1, 2))
+            e = 2.0 ** -18 * 0.125 * (a.abs() @ b.abs().transpose(1, 2)).amax(-1)
+            L = torch.logsumexp(s, -1)
+            assert torch.all((lse[lo:hi].cpu().double().transpose(0, 1) - L).abs() <= e + 2.0 ** -22 * (4 + L.abs()))
