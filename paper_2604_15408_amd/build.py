@@ -30,7 +30,7 @@ HIPCC_FLAGS = [
 # instructions (attention and the linear layers order their parameters by first use).  Measured side by side: attention and the
 # 36-kernel pipeline 2-3 % faster, linear layers over a few hundred to some thousand rows 1-2 %.
 PRELOAD = ["-mllvm", "-amdgpu-kernarg-preload-count=14"]
-PER_FILE_FLAGS = {"attn.hip": PRELOAD, "pack_unpack.hip": PRELOAD, "mask.hip": PRELOAD, "linear_f16.hip": PRELOAD,
+PER_FILE_FLAGS = {"attn.hip": PRELOAD, "attn_backward.hip": PRELOAD, "pack_unpack.hip": PRELOAD, "mask.hip": PRELOAD, "linear_f16.hip": PRELOAD,
                   "linear_bf16.hip": PRELOAD}
 
 

@@ -24,8 +24,8 @@
 // P and dS are rounded to the input type for the second products, as the gradients themselves are in the end: a sum of n terms
 // whose signs are mixed is off by about as much as its own rounding.  Sums are fp32.
 //
-// us now (gradients alone, H = 12): 32 x 577 bf16 144 (82 GFLOP in five products, 115 in the seven of this form: 0.8 PFLOP/s, where a loop of
-// products alone sustains 1.3), 64 x 197 fp16 55 (155 MB of rows: 26 us at the rate of a copy), 32 x about 40 bf16 6.7.
+// us now (gradients alone, H = 12): 32 x 577 bf16 141 (82 GFLOP in five products, 115 in the seven of this form: 0.8 PFLOP/s, where a loop of
+// products alone sustains 1.3), 64 x 197 fp16 52 (155 MB of rows: 26 us at the rate of a copy), 32 x about 40 bf16 6.7.
 #include <type_traits>
 
 #include "attn_parts.h"
@@ -44,6 +44,9 @@ constexpr int kSmallGroups = 512;
 // the forward pass, would be streamed again and again (64 x 197 tokens: 512 pairs 59 us, 256 61, 128 55; 32 x 577: 512 159, 128 154, 64 144).
 constexpr int kGroupPairs = 512, kGroupPairsMin = 32;
 constexpr int64_t kGroupBytes = 3 << 20;
+// Up to 512 pairs whose work-groups are no more than this start about together in any order, and in one batch those of them that have
+// rows are dealt out evenly: 32 x about 40 of 197 tokens 6.7 us and 7.6 in batches of 128, 32 x about 100 12.8 and 13.4, 8 x 900 83 and 86.
+constexpr int kAtOnce = 2048;
 constexpr int kSlotBytes = 3 * kTileBytes;      // tiles A and B; keys: the rows of o besides
 constexpr int kLseBytes = kBN * 4;
 constexpr int kLdsBytes = 2 * kSlotBytes + 2 * kLseBytes + 2 * kBN * 4;      // ring, L of a tile's queries, statistics (L log2 e, - delta)
@@ -52,9 +55,7 @@ struct BackwardArgs {
     const uint16_t *q, *k, *v, *o, *d_o;
     uint16_t *dq, *dk, *dv;
     const float* lse;                   // [rows, H]
-    const int32_t* cu_seqlens;
-    int H, pairs, group, in_tok, out_tok, grad_tok;
-    uint32_t h_magic;
+    int H, in_tok, out_tok, grad_tok;
     float scale;
 };
 
@@ -212,12 +213,17 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
         }
     };
 
-    // 32 rows of a tile: MASK where some of them may lie behind the last key
-    auto block = [&](uint32_t tile, int bb, int rem, auto mask) {
+    // 32 rows of a tile: MASK where some of them may lie behind the last key, NU = 1 where the second 16 all do
+    auto block = [&](uint32_t tile, int bb, int rem, auto mask, auto subtiles) {
         constexpr bool MASK = decltype(mask)::value;
+        constexpr int NU = decltype(subtiles)::value;
         f32x4 pr[CB][2], ds[CB][2];
+        if (NU == 1) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+            for (int cb = 0; cb < CB; ++cb) pr[cb][1] = ds[cb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
             const int kt = 2 * bb + u;
             const uint32_t ra = tile + row_rel + kt * 16 * 128, rb = ra + kTileBytes;
             const vec8 a0 = as_vec8<vec8>(lds_read16(ra)), a1 = as_vec8<vec8>(lds_read16(ra ^ 16u));
@@ -277,13 +283,19 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
         if (active) {
             const uint32_t tile = ring0 + slot * kSlotBytes;
             const int rem = n - t * kBN;
+            typedef std::integral_constant<int, 1> Half;
+            typedef std::integral_constant<int, 2> Whole;
+            // a last block of at most 16 rows has a form of its own: 64 x 197 tokens 57.4 -> 54.7 us (CB = 1, a chain of latencies, gains nothing)
+            const int whole = rem >= kBN ? 2 : CB == 1 ? (rem + 31) >> 5 : (rem + 15) >> 5;
             if (KEYS || rem >= kBN) {
-                const int blocks = rem > 32 ? 2 : 1;
 #pragma nounroll
-                for (int bb = 0; bb < blocks; ++bb) block(tile, bb, rem, std::false_type{});
+                for (int bb = 0; bb < whole; ++bb) block(tile, bb, rem, std::false_type{}, Whole{});
             } else {
 #pragma nounroll
-                for (int bb = 0; 32 * bb < rem; ++bb) block(tile, bb, rem, std::true_type{});
+                for (int bb = 0; bb < whole; ++bb) block(tile, bb, rem, std::true_type{}, Whole{});
+            }
+            if constexpr (CB > 1) {
+                if (32 * whole < rem && rem < kBN) block(tile, whole, rem, std::true_type{}, Half{});
             }
         }
     }
@@ -420,20 +432,22 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
 
 template <typename In, int CB>
 __global__ __launch_bounds__(kBlockThreads, 3)             // three work-groups on a CU: 168 registers, 49 KB of LDS
-void attn_backward_kernel(BackwardArgs p) {
+void attn_backward_kernel(const int32_t* __restrict__ cu_seqlens, int H, uint32_t h_magic, int pairs, int group, int own_tiles, BackwardArgs p) {
+    // (what a work-group needs to find out whether it has rows at all arrives in scalar registers with its wavefronts)
     __shared__ __attribute__((aligned(1024))) uint4 lds[kLdsBytes / 16];
-    const int pair = blockIdx.z * p.group + blockIdx.x;
-    if (pair >= p.pairs) return;
+    const int pair = blockIdx.z * group + blockIdx.x;
+    if (pair >= pairs) return;
     uint32_t img, h;
-    divmod((uint32_t)pair, (uint32_t)p.H, p.h_magic, img, h);
-    const int s = p.cu_seqlens[img], n = __builtin_amdgcn_readfirstlane(p.cu_seqlens[img + 1] - s);
-    const int m0 = (blockIdx.y >> 1) * 64 * CB;
+    divmod((uint32_t)pair, (uint32_t)H, h_magic, img, h);
+    const int s = cu_seqlens[img], n = __builtin_amdgcn_readfirstlane(cu_seqlens[img + 1] - s);
+    const int y = (int)blockIdx.y, tile = y >= own_tiles ? y - own_tiles : y;     // keys, which take longer, first
+    const int m0 = tile * 64 * CB;
     if (m0 >= n) return;
-    if (n <= kBN) {
-        if (blockIdx.y == 0) whole_sequence<In>(p, lds, s, n, (int)h);
+    if (__builtin_expect(n <= kBN, 1)) {
+        if (y == 0) whole_sequence<In>(p, lds, s, n, (int)h);
         return;
     }
-    if (blockIdx.y & 1) own_rows<In, false, CB>(p, lds, s, n, (int)h, m0);
+    if (y != tile) own_rows<In, false, CB>(p, lds, s, n, (int)h, m0);
     else own_rows<In, true, CB>(p, lds, s, n, (int)h, m0);
 }
 
@@ -445,19 +459,19 @@ hipError_t launch_attn_backward(const void* q, const void* k, const void* v, con
     const int pairs = B * H;
     const int own = (int64_t)pairs * 2 * ((max_seqlen + 127) / 128) <= kSmallGroups ? 64 : 128, tiles = (max_seqlen + own - 1) / own;
     int group = kGroupPairs;
-    while (group > kGroupPairsMin && (int64_t)group / kXcds * max_seqlen * (5 * kHeadDim * 2) > kGroupBytes) group /= 2;
+    const bool at_once = pairs <= kGroupPairs && pairs * 2 * tiles <= kAtOnce;
+    while (!at_once && group > kGroupPairsMin && (int64_t)group / kXcds * max_seqlen * (5 * kHeadDim * 2) > kGroupBytes) group /= 2;
     while ((pairs + group - 1) / group > kMaxGridYZ) group *= 2;              // (ends: the C ABI layer has checked it for 512)
     const int pairs8 = (pairs + kXcds - 1) / kXcds * kXcds;
     if (group > pairs8) group = pairs8;
     const int batches = (pairs + group - 1) / group;
     const BackwardArgs p{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v),
                          static_cast<const uint16_t*>(o), static_cast<const uint16_t*>(d_o), static_cast<uint16_t*>(dq),
-                         static_cast<uint16_t*>(dk), static_cast<uint16_t*>(dv), lse, cu_seqlens, H, pairs, group, (int)in_tok, (int)out_tok,
-                         (int)grad_tok, div_magic((uint32_t)H), scale};
+                         static_cast<uint16_t*>(dk), static_cast<uint16_t*>(dv), lse, H, (int)in_tok, (int)out_tok, (int)grad_tok, scale};
     const dim3 grid(group, 2 * tiles, batches);
     auto typed = [&](auto in) {
         typedef decltype(in) In;
-        return launch_kernel(own == 64 ? attn_backward_kernel<In, 1> : attn_backward_kernel<In, 2>, grid, dim3(kBlockThreads), stream, p);
+        return launch_kernel(own == 64 ? attn_backward_kernel<In, 1> : attn_backward_kernel<In, 2>, grid, dim3(kBlockThreads), stream, cu_seqlens, H, div_magic((uint32_t)H), pairs, group, tiles, p);
     };
     return dt == RAGGED_F16 ? typed(F16{}) : typed(BF16{});
 }
