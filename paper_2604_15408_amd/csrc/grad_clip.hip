@@ -8,7 +8,7 @@
 // Squares are formed and added in fp64: they are exact there (24-bit values), no gradient's square overflows or vanishes,
 // and with one conversion and one fma a value the kernel stays bound by memory.
 //
-// us (both kernels): 151 M bf16 values into fp32 206 (squares 46: 6.6 TB/s; scaling 160: 5.7 TB/s of reads and writes), fp32 into fp32 317;
+// us (both kernels): 151 M bf16 values into fp32 194 (squares 46: 6.6 TB/s; scaling 148: 6.1 TB/s of reads and writes), fp32 into fp32 304;
 // 5.5 M fp32 values 16.4 (5.3 and 9.0 in the kernels); 180 thousand 9.
 #include "common.h"
 #include "linear_kernel.h"
@@ -17,7 +17,8 @@ namespace ragged {
 namespace {
 
 constexpr int kChunk = 16384;                                  // values of a chunk (151 M bf16 into fp32: 8192 as fast, 32768 213 us)
-// Outputs of more values than this go past the caches, which keeps the gradients there for the second reading: 151 M values 242 -> 206 us.
+// Outputs of more values than this go past the caches, which keeps the gradients there for the second reading: 151 M values 242 -> 206 us;
+// that one then leaves them to others as well: 194.
 // Fewer are left there for the optimiser (38 M into fp32 55 us, 53 past them).
 constexpr int64_t kClipBypass = 32 << 20;
 constexpr int kClipGroups = 1024;                              // work-groups (and partial sums) at most
@@ -55,6 +56,9 @@ struct GradLine {
     typedef __attribute__((address_space(1))) word global_word;
     static __device__ __forceinline__ line load(const void* p, int i) {
         return *(const global_line*)((const global_word*)p + i);
+    }
+    static __device__ __forceinline__ line load_last(const void* p, int i) {
+        return __builtin_nontemporal_load((const global_line*)((const global_word*)p + i));
     }
     static __device__ __forceinline__ word load1(const void* p, int i) { return ((const global_word*)p)[i]; }
     static __device__ __forceinline__ void store1(void* p, int i, word w) { ((global_word*)p)[i] = w; }
@@ -138,7 +142,7 @@ __device__ __forceinline__ void chunk_scale(const void* src, void* dst, int n, f
     for (; i + (kClipAhead - 1) * kStep < whole; i += kClipAhead * kStep) {
         typename In::line w[kClipAhead];
 #pragma unroll
-        for (int u = 0; u < kClipAhead; ++u) w[u] = In::load(src, i + u * kStep);
+        for (int u = 0; u < kClipAhead; ++u) w[u] = BYPASS ? In::load_last(src, i + u * kStep) : In::load(src, i + u * kStep);
 #pragma unroll
         for (int u = 0; u < kClipAhead; ++u) scale(w[u], i + u * kStep);
     }

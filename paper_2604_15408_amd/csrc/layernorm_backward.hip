@@ -6,7 +6,9 @@
 //   columns in all the rows that it takes and adds up their share of dgamma and dbeta in registers; a work-group adds those of its
 //   lanes up through LDS and leaves one partial sum for each column in the workspace.
 // layernorm_sums_kernel: adds up the partial sums of the work-groups, always in the same order.
-// Bound by memory: x, dy and res in, dx out.
+// Bound by memory: x, dy and res in, dx out.  25 216 x 1024 fp16 with residual (206 MB) 37 us over and over, of which 33 the rows, 42 from HBM.
+#include <type_traits>
+
 #include "common.h"
 #include "lane_sums.h"
 #include "linear_kernel.h"
@@ -17,9 +19,17 @@ namespace {
 constexpr int kLnbGroups = 512;                                // work-groups at most: two on a CU
 constexpr int kSumThreads = 1024, kSumColumns = 32;
 
-__host__ __device__ inline int64_t lnb_rows_at_once(int lanes) { return kBlockThreads / lanes; }
+template <int AUX>
+__device__ __forceinline__ LinearLine<8> load_chunk(__amdgpu_buffer_rsrc_t rsrc, uint32_t voff) {
+    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, voff, 0, AUX);
+    return __builtin_bit_cast(LinearLine<8>, v);
+}
 
-template <typename In, int L, int NC>
+// LAST: loads and stores that leave the caches to others.  Nothing of the inputs is used again; from HBM, with residual, 25 216 x 1024 47 us
+// without and 42 with it, 12 608 x 2048 49 and 44, without residual 25 216 x 768 30.5 and 28, and with a kernel that reads dx next 56.5 / 52.4,
+// 58.6 / 54.6, 37.4 / 35.8.  Smaller tensors, mostly still in the caches from the kernel that wrote them, gain nothing (25 216 x 192 17.5 / 18.2).
+constexpr int64_t kLnbLast = 32 << 20;                         // bytes of dx from which on
+template <typename In, int L, int NC, bool LAST>
 __global__ __launch_bounds__(kBlockThreads)
 void layernorm_backward_kernel(const uint16_t* __restrict__ x, const uint16_t* __restrict__ gamma, const uint16_t* dy, const uint16_t* res,
                                uint16_t* dx, float* __restrict__ partial, int rows_cap, const int32_t* __restrict__ rows_dev, int C,
@@ -27,6 +37,7 @@ void layernorm_backward_kernel(const uint16_t* __restrict__ x, const uint16_t* _
     typedef LinearLine<8> Chunk;
     constexpr int kRows = kWaveSize / L;                       // rows of a wavefront at a time
     constexpr int kGroupRows = kBlockThreads / L;              // rows of a work-group at a time
+    constexpr int kAux = LAST ? 2 : 0;                         // the non-temporal bit of a buffer access
     __shared__ float sums[NC * 8 * kBlockThreads];
     int given = rows_cap;
     if (rows_dev) { const int r = *rows_dev; given = r < given ? r : given; }
@@ -53,13 +64,13 @@ void layernorm_backward_kernel(const uint16_t* __restrict__ x, const uint16_t* _
         Chunk x_raw[NC], dy_raw[NC], res_raw[NC];
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            x_raw[i] = Chunk::load(x_rsrc, offset(i, lane_row));
-            dy_raw[i] = Chunk::load(dy_rsrc, offset(i, lane_row));
+            x_raw[i] = load_chunk<kAux>(x_rsrc, offset(i, lane_row));
+            dy_raw[i] = load_chunk<kAux>(dy_rsrc, offset(i, lane_row));
         }
         if (res) {
             const __amdgpu_buffer_rsrc_t res_rsrc = buf_rsrc(res + row * C, records);
 #pragma unroll
-            for (int i = 0; i < NC; ++i) res_raw[i] = Chunk::load(res_rsrc, offset(i, lane_row));
+            for (int i = 0; i < NC; ++i) res_raw[i] = load_chunk<kAux>(res_rsrc, offset(i, lane_row));
         }
         float v[NC][8], sum = 0.f;
 #pragma unroll
@@ -106,7 +117,7 @@ void layernorm_backward_kernel(const uint16_t* __restrict__ x, const uint16_t* _
             if (res) res_raw[i].unpack(In{}, add);
 #pragma unroll
             for (int e = 0; e < 8; ++e) out[e] = __builtin_fmaf(rstd, w[i][e] - s1 - v[i][e] * s2, add[e]);
-            Chunk::pack(In{}, out).store(dx_rsrc, offset(i, lane_row));
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, Chunk::pack(In{}, out)), dx_rsrc, offset(i, lane_row), 0, kAux);
         }
     }
     // the lanes of the work-group that share a column: one value each, column sub + L i of lane-row threadIdx / L
@@ -176,13 +187,17 @@ hipError_t launch_layernorm_backward(const void* x, const void* gamma, const voi
                              static_cast<const uint16_t*>(gamma), static_cast<const uint16_t*>(dy), static_cast<const uint16_t*>(res),
                              static_cast<uint16_t*>(dx), partial, rows_cap, rows_dev, C, eps);
     };
-    auto typed = [&](auto in) {
+    const int chunks = (C / 8 + shape.lanes - 1) / shape.lanes;
+    auto form = [&](auto in, auto last) {
         typedef decltype(in) In;
-        const int chunks = (C / 8 + shape.lanes - 1) / shape.lanes;
-        if (shape.lanes == 16) return chunks == 1 ? launch(layernorm_backward_kernel<In, 16, 1>) : launch(layernorm_backward_kernel<In, 16, 2>);
-        if (shape.lanes == 32) return chunks == 2 ? launch(layernorm_backward_kernel<In, 32, 2>) : launch(layernorm_backward_kernel<In, 32, 3>);
-        return chunks == 2 ? launch(layernorm_backward_kernel<In, 64, 2>)
-             : chunks == 3 ? launch(layernorm_backward_kernel<In, 64, 3>) : launch(layernorm_backward_kernel<In, 64, 4>);
+        constexpr bool LAST = decltype(last)::value;
+#define LNB_FORM(L, NC) if (shape.lanes == L && chunks == NC) return launch(layernorm_backward_kernel<In, L, NC, LAST>);
+        LNB_FORM(16, 1) LNB_FORM(16, 2) LNB_FORM(32, 2) LNB_FORM(32, 3) LNB_FORM(64, 2) LNB_FORM(64, 3)
+        return launch(layernorm_backward_kernel<In, 64, 4, LAST>);
+#undef LNB_FORM
+    };
+    auto typed = [&](auto in) {
+        return (int64_t)rows_cap * C * 2 > kLnbLast ? form(in, std::true_type{}) : form(in, std::false_type{});
     };
     const hipError_t err = dt == RAGGED_F16 ? typed(F16{}) : typed(BF16{});
     if (err != hipSuccess) return err;

@@ -21,8 +21,8 @@ template <> struct Words<1> { typedef uint16_t type; };
 constexpr int kRopeAhead = 4;                                  // units a thread requests before the angles are there
 constexpr int kRopeRows = 64;                                  // rows of a work-group at most
 constexpr int kRopeAngles = 2048;                              // angles of a work-group at most (16 KB of LDS)
-// Output beyond half of the last-level cache goes past it: 168 MB alone 51 us instead of 75 over and over, 72 instead of 77 from HBM, and
-// with a kernel that reads it next 104 instead of 102.  Below, the next kernel finds it there (57 MB: 27 us and 38 with its reader either way).
+// Output beyond half of the last-level cache goes past it, and so do the inputs, which nothing reads again: 168 MB alone 51 us instead of 75 over
+// and over, 70 instead of 77 from HBM, and with a kernel that reads it next 104 instead of 102.  Below, the next kernel finds it there (57 MB: 27 us and 38 with its reader either way).
 constexpr int64_t kRopeBypass = 128 << 20;                     // bytes
 constexpr int kRopeFill = 512;                                 // work-groups below which rows are not gathered into fewer
 
@@ -107,16 +107,20 @@ void rope_kernel(RopeArgs p) {
     // interleaved: what rotates and what is copied lie in one row of equal lines; half: a unit has two lines, a copied one a line of its own width
     struct Values { Line a, b; };
     static_assert(sizeof(CopyLine) <= sizeof(Values), "a copied unit's values are kept in place of a pair's");
+    auto get = [&](auto* src) {
+        if constexpr (BYPASS) return __builtin_nontemporal_load(src);
+        else return *src;
+    };
     auto load = [&](const Place& at) {
         Values v;
         const uint32_t j = at.piece;
         if (LAYOUT == kInterleaved) {
-            v.a = *reinterpret_cast<const Line*>(at.src + W * j);
+            v.a = get(reinterpret_cast<const Line*>(at.src + W * j));
         } else if (j < (uint32_t)p.rotated) {
-            v.a = *reinterpret_cast<const Line*>(at.src + W * j);
-            v.b = *reinterpret_cast<const Line*>(at.src + W * j + p.pairs);
+            v.a = get(reinterpret_cast<const Line*>(at.src + W * j));
+            v.b = get(reinterpret_cast<const Line*>(at.src + W * j + p.pairs));
         } else {
-            const CopyLine c = *reinterpret_cast<const CopyLine*>(at.src + 2 * p.pairs + CW * (j - p.rotated));
+            const CopyLine c = get(reinterpret_cast<const CopyLine*>(at.src + 2 * p.pairs + CW * (j - p.rotated)));
             __builtin_memcpy(&v, &c, sizeof(c));
         }
         return v;

@@ -128,3 +128,22 @@ def test_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((dx, dgamma, dbeta), want))
+
+
+@pytest.mark.parametrize("C,rows", [(128, 140001), (256, 70003), (512, 33001), (768, 22003), (1024, 17001), (1536, 11003)])
+def test_tensors_larger_than_the_caches(C, rows):
+    """More than 32 MB a tensor: the same bits of dx as in pieces, and the sums of the formulas."""
+    gen = torch.Generator(device=DEV).manual_seed(C + 1)
+    x, dy, res = (torch.randn(rows, C, generator=gen, device=DEV).add(0.5).half() for _ in range(3))
+    gamma = torch.randn(C, generator=gen, device=DEV).half()
+    dx, want = torch.empty_like(x), torch.empty_like(x)
+    (dgamma, dbeta), spare = torch.empty(2, C, device=DEV), torch.empty(C, device=DEV)
+    workspace = torch.empty(binding.layernorm_backward_workspace(rows, C), dtype=torch.uint8, device=DEV)
+    binding.ragged_layernorm_backward(x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad=res)
+    for lo in range(0, rows, 7000):
+        s = slice(lo, min(lo + 7000, rows))
+        binding.ragged_layernorm_backward(x[s], gamma, dy[s], want[s], spare, spare.clone(), workspace, residual_grad=res[s])
+    assert torch.equal(dx, want)
+    _, _, wg, sg, wb, sb = _reference(x, gamma, dy, None, 1e-6)
+    # (a column's values pass up to 500 additions here: 500 * 2^-24 = 3e-5 of the sum of sizes, and the error of xh)
+    assert torch.all((dgamma.double() - wg).abs() <= 5e-5 * sg) and torch.all((dbeta.double() - wb).abs() <= 4e-5 * sb)
