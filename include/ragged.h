@@ -309,7 +309,8 @@ int ragged_keep_topk(const double* scores, int B, int N, int k, uint8_t* keep, v
  *
  *   q, q_out   [rows, Hq, D]  rows q_stride / q_out_stride elements apart, [Hq, D] contiguous inside a row (dt)
  *   k, k_out   [rows, Hk, D]  the same with k_stride / k_out_stride and their own number of heads; both NULL: no keys
- *              q_out may be q (then with the same stride) and k_out may be k; other overlaps are not allowed
+ *              q_out may be q (then with the same stride) and k_out may be k; other overlaps are not allowed (q_out = k, k_out = q and
+ *              q_out = k_out are refused, RAGGED_ERR_UNSUPPORTED)
  *   rows_cap, rows_dev        as for ragged_linear
  *   coords     [n_coords, axes]  fp32 positions; row r has those of line  u mod n_coords,  u = index[r] as an unsigned number
  *                             (index NULL: r itself).  Packed rows of images pass gather_idx and the N tokens' coordinates, text passes
@@ -355,7 +356,8 @@ int ragged_attn_lse(const void* q, const void* k, const void* v, void* o, float*
  *   o, d_o     [T, H, D]  its output and that output's gradient, out_tok_stride elements between tokens
  *   lse        [T, H]     as it wrote them
  *   dq, dk, dv [T, H, D]  out (dt), grad_tok_stride elements between tokens (for example the slices of a fused [T, 3, H, D] buffer);
- *                         they must not overlap any input.  Rows >= T are left untouched
+ *                         they must not overlap any input or each other (the same address is refused, RAGGED_ERR_UNSUPPORTED).  Rows >= T
+ *                         are left untouched
  *   max_seqlen            an upper bound on every n_i; gradients of rows at positions >= max_seqlen of a longer sequence may be left
  *                         uncomputed (such a row then stays untouched as a whole)
  *

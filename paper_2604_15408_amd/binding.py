@@ -601,6 +601,7 @@ class GradPlan:
                 raise ValueError("all tensors must be on one device")
             if o is not None:
                 e.dst, e.dst_dt = _dev(o, "out", (g.dtype, torch.float32), tuple(g.shape)), _DTYPE_CODE[o.dtype]
+        self._refuse_overlaps(grads, outs)
         chunks = ctypes.c_int64()
         plan = lambda table, size: _check("ragged_grad_plan", _native().ragged_grad_plan(
             ctypes.addressof(entries), len(grads), table, size, ctypes.addressof(chunks)))
@@ -611,6 +612,26 @@ class GradPlan:
         self.table = host.to(grads[0].device)
         self.workspace = torch.empty(GRAD_WORKSPACE, dtype=torch.uint8, device=grads[0].device)
         self.tensors = (grads, outs)
+
+
+    @staticmethod
+    def _refuse_overlaps(grads, outs):
+        """No output may lie over another one or over a gradient that is not its own (all of it): they are read and written in any order."""
+        span = lambda t: (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+        written, read = [], []
+        for g, o in zip(grads, outs):
+            if g.numel() == 0:
+                continue
+            if o is not None:
+                written.append((*span(o), True))
+            if o is None or span(o) != span(g):
+                read.append((*span(g), False))
+        end, last_written = 0, 0                               # how far any span so far reaches, and any written one
+        for lo, hi, is_written in sorted(written + read, key=lambda s: s[:2]):
+            if lo < (end if is_written else last_written):
+                raise ValueError("outputs overlap each other or gradients that are not their own")
+            end = max(end, hi)
+            last_written = max(last_written, hi) if is_written else last_written
 
 
 def _grad_clip_args(plan, norm, max_norm, scale, stream):

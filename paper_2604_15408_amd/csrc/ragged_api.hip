@@ -228,6 +228,7 @@ int ragged_rope(const void* q, const void* k, void* q_out, void* k_out, int64_t 
     if (!is16bit(dt) || (D & 7) != 0 || D > 512 || (layout != 0 && layout != 1) || (inverse != 0 && inverse != 1) || !isfinite(amplitude))
         return RAGGED_ERR_UNSUPPORTED;
     if ((q_stride & 7) != 0 || (q_out_stride & 7) != 0 || (k && ((k_stride & 7) != 0 || (k_out_stride & 7) != 0))) return RAGGED_ERR_UNSUPPORTED;
+    if (k && (q_out == k || k_out == q || q_out == k_out)) return RAGGED_ERR_UNSUPPORTED;      // one would be read after the other is written
     if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned4(coords) || !aligned4(index) || !aligned4(rows_dev) ||
         !aligned8(freqs))
         return RAGGED_ERR_UNSUPPORTED;
@@ -277,6 +278,11 @@ int ragged_attn_backward(const void* q, const void* k, const void* v, const void
     if (out_tok_stride > (int64_t)1 << 23 || grad_tok_stride < (int64_t)H * D || grad_tok_stride > (int64_t)INT32_MAX) return RAGGED_ERR_SHAPE;
     if ((grad_tok_stride & 7) != 0 || !aligned4(lse)) return RAGGED_ERR_UNSUPPORTED;
     if (!aligned16(d_o) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv)) return RAGGED_ERR_UNSUPPORTED;
+    // other work-groups still read the inputs when the first gradients are written
+    for (const void* out : {dq, dk, dv})
+        for (const void* in : {q, k, v, o, d_o})
+            if (out == in) return RAGGED_ERR_UNSUPPORTED;
+    if (dq == dk || dq == dv || dk == dv) return RAGGED_ERR_UNSUPPORTED;
     return from_hip(ragged::launch_attn_backward(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, B, max_seqlen, H, in_tok_stride, out_tok_stride,
                                                  grad_tok_stride, scale, dt, static_cast<hipStream_t>(stream)));
 }

@@ -32,7 +32,7 @@ def test_rope_validation(lib):
         assert call(**bad) == SHAPE, bad
     for bad in (dict(dt=2), dict(d=60, pairs=30), dict(d=520, qs=1040, qos=1040, ks=520, kos=520), dict(layout=2), dict(inv=2),
                 dict(amp=float("nan")), dict(qs=132), dict(kos=68), dict(q=FAKE + 8), dict(ko=FAKE + 2), dict(fr=FAKE + 4), dict(co=FAKE + 2),
-                dict(ix=FAKE + 1), dict(rd=FAKE + 2)):
+                dict(ix=FAKE + 1), dict(rd=FAKE + 2), dict(k=FAKE * 2), dict(q=FAKE * 3), dict(ko=FAKE * 2)):
         assert call(**bad) == UNSUPPORTED, bad
 
 
@@ -48,8 +48,8 @@ def test_attn_lse_validation(lib):
 
 
 def test_attn_backward_validation(lib):
-    def call(q=FAKE, k=FAKE, v=FAKE, o=FAKE, do=FAKE, lse=FAKE, dq=FAKE, dk=FAKE, dv=FAKE, cu=FAKE, B=2, ms=8, H=2, D=64, si=384, so=128,
-             sg=384, scale=0.125, dt=0):
+    def call(q=FAKE, k=FAKE, v=FAKE, o=FAKE, do=FAKE, lse=FAKE, dq=2 * FAKE, dk=3 * FAKE, dv=4 * FAKE, cu=FAKE, B=2, ms=8, H=2, D=64, si=384,
+             so=128, sg=384, scale=0.125, dt=0):
         return lib.ragged_attn_backward(q, k, v, o, do, lse, dq, dk, dv, cu, B, ms, H, D, si, so, sg, scale, dt, None)
     for null in ("q", "k", "v", "o", "do", "lse", "dq", "dk", "dv", "cu"):
         assert call(**{null: None}) == NULL
@@ -57,7 +57,8 @@ def test_attn_backward_validation(lib):
                 dict(si=127), dict(so=64), dict(sg=120), dict(so=(1 << 23) + 8), dict(sg=1 << 31)):
         assert call(**bad) == SHAPE, bad
     for bad in (dict(D=128, si=768, so=256, sg=768), dict(si=132), dict(so=132), dict(sg=132), dict(dt=2), dict(scale=float("nan")),
-                dict(lse=FAKE + 2), dict(do=FAKE + 8), dict(dq=FAKE + 2), dict(dk=FAKE + 4), dict(dv=FAKE + 8)):
+                dict(lse=FAKE + 2), dict(do=FAKE + 8), dict(dq=FAKE + 2), dict(dk=FAKE + 4), dict(dv=FAKE + 8), dict(dq=FAKE),
+                dict(dk=FAKE), dict(dv=FAKE), dict(o=5 * FAKE, dv=5 * FAKE), dict(dk=2 * FAKE), dict(dv=3 * FAKE)):
         assert call(**bad) == UNSUPPORTED, bad
 
 
@@ -151,6 +152,29 @@ def test_rope_frequencies(lib):
     assert call(p=ctypes.addressof(out), length=0.0) == 0
     with pytest.raises(ValueError):
         binding.rope_frequencies(5, axes=2)
+
+
+def test_native_checks_of_rows_and_devices(lib):
+    native = binding._native()
+    t = torch.zeros(4, 2, 64, dtype=torch.float16)
+    for other in (t, torch.nn.Parameter(t), None, 3):
+        assert native.rows(other, None, None) is None
+    assert native.here(-1, t, None) and not native.here(0, t) and not native.here(-1, t, "x") and native.here(0)
+    with pytest.raises(TypeError):
+        native.rows(t)
+
+
+def test_grad_outputs_that_overlap_are_refused(monkeypatch):
+    """Two tensors that would be written to the same place, or one over another's gradient (addresses stand in for GPU tensors)."""
+    monkeypatch.setattr(binding, "_dev", lambda t, *rest: t.data_ptr())
+    flat = torch.zeros(100)
+    for grads, outs in (([flat[:50], flat[:50]], None), ([flat[:60], flat[50:]], None), ([flat[:50], flat[50:]], [flat[:50], flat[:50]]),
+                        ([flat[:50], flat[50:]], [flat[50:], None]), ([flat[:50]], [flat[1:51]])):
+        with pytest.raises(ValueError, match="overlap"):
+            binding.GradPlan(grads, outs)
+    binding.GradPlan([flat[:50], flat[:50]], [None, None])     # (nothing is written)
+    binding.GradPlan([flat[:50], flat[50:]])
+    binding.GradPlan([flat[:0], flat[:50]], [flat[:0], torch.zeros(50)])
 
 
 def test_binding_refuses_before_the_library():
