@@ -442,26 +442,32 @@ def rope_frequencies(pairs: int, base: float = 10000.0, axes: int = 1, scaling: 
 
 
 def _rope_args(q, k, q_out, k_out, coords, freqs, index, layout, amplitude, inverse, rows_dev, stream):
+    native = _marshal or _native()
+    rows, dev = native.rows, native.dev
+    dt, shape = q.dtype, q.shape
     if (k is None) != (k_out is None):
         raise ValueError("k and k_out come together")
-    qp, qs = _token_rows(q, "q", _HALF, None)
-    qop, qos = _token_rows(q_out, "q_out", q.dtype, q.shape)
-    rows, hq, d = q.shape
+    qp, qs = rows(q, _HALF, None) or _token_rows(q, "q", _HALF, None)
+    qop, qos = rows(q_out, dt, shape) or _token_rows(q_out, "q_out", dt, shape)
+    n, hq, d = shape
     kp = kop = None
     hk = ks = kos = 0
     if k is not None:
-        kp, ks = _token_rows(k, "k", q.dtype, None)
-        kop, kos = _token_rows(k_out, "k_out", q.dtype, k.shape)
-        hk = k.shape[1]
-        if k.shape[0] != rows or k.shape[2] != d:
-            raise ValueError(f"k has shape {tuple(k.shape)}, expected [{rows}, heads, {d}]")
+        kp, ks = rows(k, dt, None) or _token_rows(k, "k", dt, None)
+        kop, kos = rows(k_out, dt, k.shape) or _token_rows(k_out, "k_out", dt, k.shape)
+        kn, hk, kd = k.shape
+        if kn != n or kd != d:
+            raise ValueError(f"k has shape {tuple(k.shape)}, expected [{n}, heads, {d}]")
     if coords.dim() != 2:
         raise ValueError("coords must be [n, axes]")
+    lines, axes = coords.shape
+    args = (qp, kp, qop, kop, n, None if rows_dev is None else _rows_dev(rows_dev), hq, hk, d, qs, ks, qos, kos,
+            dev(coords, torch.float32, None) or _dev(coords, "coords", torch.float32), lines, axes,
+            None if index is None else dev(index, torch.int32, (n,)) or _dev(index, "index", torch.int32, (n,)),
+            dev(freqs, torch.float64, None) or _dev(freqs, "freqs", torch.float64), freqs.numel(), _ROPE_LAYOUT[layout], float(amplitude),
+            1 if inverse else 0, _DTYPE_CODE[dt], _stream(stream))
     _here(q, k, q_out, k_out, coords, freqs, index, rows_dev)
-    return (qp, kp, qop, kop, rows, _rows_dev(rows_dev), hq, hk, d, qs, ks, qos, kos, _dev(coords, "coords", torch.float32),
-            coords.shape[0], coords.shape[1], None if index is None else _dev(index, "index", torch.int32, (rows,)),
-            _dev(freqs, "freqs", torch.float64), freqs.numel(), _ROPE_LAYOUT[layout], float(amplitude), int(bool(inverse)),
-            _DTYPE_CODE[q.dtype], _stream(stream))
+    return args
 
 
 def ragged_rope(q, k, q_out, k_out, coords, freqs, index=None, layout: str = "half", amplitude: float = 1.0, inverse: bool = False,
@@ -491,7 +497,9 @@ def _attn_lse_args(q, k, v, o, lse, cu_seqlens, max_seqlen, scale, stream):
         raise ValueError("q, k, v must share their token stride")
     _here(q, k, v, o, lse, cu_seqlens)
     n, H, D = shape
-    return (qp, kp, vp, op, _dev(lse, "lse", torch.float32, (n, H)), _dev(cu_seqlens, "cu_seqlens", torch.int32),
+    dev = (_marshal or _native()).dev
+    return (qp, kp, vp, op, dev(lse, torch.float32, (n, H)) or _dev(lse, "lse", torch.float32, (n, H)),
+            dev(cu_seqlens, torch.int32, None) or _dev(cu_seqlens, "cu_seqlens", torch.int32),
             cu_seqlens.numel() - 1, int(max_seqlen), H, D, in_tok, out_tok, float(scale), _DTYPE_CODE[dt], _stream(stream))
 
 
@@ -520,7 +528,9 @@ def _attn_backward_args(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen
         raise ValueError("q, k, v must share their token stride, o and d_o theirs, dq, dk, dv theirs")
     _here(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens)
     n, H, D = shape
-    return (qp, kp, vp, op, dop, _dev(lse, "lse", torch.float32, (n, H)), dqp, dkp, dvp, _dev(cu_seqlens, "cu_seqlens", torch.int32),
+    dev = (_marshal or _native()).dev
+    return (qp, kp, vp, op, dop, dev(lse, torch.float32, (n, H)) or _dev(lse, "lse", torch.float32, (n, H)), dqp, dkp, dvp,
+            dev(cu_seqlens, torch.int32, None) or _dev(cu_seqlens, "cu_seqlens", torch.int32),
             cu_seqlens.numel() - 1, int(max_seqlen), H, D, in_tok, out_tok, grad_tok, float(scale), _DTYPE_CODE[dt], _stream(stream))
 
 
@@ -547,14 +557,19 @@ def layernorm_backward_workspace(rows: int, C: int) -> int:
 
 
 def _layernorm_backward_args(x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad, rows_dev, eps, stream):
-    rows, C = x.shape
+    dev = (_marshal or _native()).dev
+    dt, shape = x.dtype, x.shape
+    rows, C = shape
     need = layernorm_backward_workspace(rows, C)
     if workspace.numel() * workspace.element_size() < need:
         raise ValueError(f"workspace has {workspace.numel() * workspace.element_size()} bytes, {need} are needed")
-    args = (_dev(x, "x", _HALF), _dev(gamma, "gamma", x.dtype, (C,)), _dev(dy, "dy", x.dtype, (rows, C)),
-            None if residual_grad is None else _dev(residual_grad, "residual_grad", x.dtype, (rows, C)), _dev(dx, "dx", x.dtype, (rows, C)),
-            _dev(dgamma, "dgamma", torch.float32, (C,)), _dev(dbeta, "dbeta", torch.float32, (C,)), _dev(workspace, "workspace"), rows,
-            _rows_dev(rows_dev), C, float(eps), _DTYPE_CODE[x.dtype], _stream(stream))
+    args = (dev(x, _HALF, None) or _dev(x, "x", _HALF), dev(gamma, dt, (C,)) or _dev(gamma, "gamma", dt, (C,)),
+            dev(dy, dt, shape) or _dev(dy, "dy", dt, shape),
+            None if residual_grad is None else dev(residual_grad, dt, shape) or _dev(residual_grad, "residual_grad", dt, shape),
+            dev(dx, dt, shape) or _dev(dx, "dx", dt, shape), dev(dgamma, torch.float32, (C,)) or _dev(dgamma, "dgamma", torch.float32, (C,)),
+            dev(dbeta, torch.float32, (C,)) or _dev(dbeta, "dbeta", torch.float32, (C,)),
+            dev(workspace, None, None) or _dev(workspace, "workspace"), rows, None if rows_dev is None else _rows_dev(rows_dev), C, float(eps),
+            _DTYPE_CODE[dt], _stream(stream))
     _here(x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad, rows_dev)
     return args
 
