@@ -216,3 +216,27 @@ def test_lse_leaves_the_output_as_it_is(dtype):
             e = 2.0 ** -18 * 0.125 * (a.abs() @ b.abs().transpose(1, 2)).amax(-1)
             L = torch.logsumexp(s, -1)
             assert torch.all((lse[lo:hi].cpu().double().transpose(0, 1) - L).abs() <= e + 2.0 ** -22 * (4 + L.abs()))
+
+
+def test_rows_far_apart():
+    """Token rows 4 MB apart: the last ones lie beyond 2^32 bytes of their tensors."""
+    lengths, H, far = [600, 1, 499], 2, 1 << 21
+    rows, q, k, v, do, cu = _inputs(lengths, H, "bf16", 21, extra=0)
+    want = _run(q, k, v, do, cu, 600, 0.125)
+
+    def apart(n):
+        buffer = torch.empty((rows - 1) * far + n * H * D, dtype=q.dtype, device=DEV)
+        return [buffer.as_strided((rows, H, D), (far, D, 1), i * H * D) for i in range(n)]
+    ins, outs, grads = apart(3), apart(2), apart(3)
+    for a, b in zip((*ins, outs[1]), (q, k, v, do)):
+        a.copy_(b)
+    lse = torch.zeros(rows, H, device=DEV)
+    binding.ragged_attn_lse(*ins, outs[0], lse, cu, 600, 0.125)
+    binding.ragged_attn_backward(*ins, *outs, lse, *grads, cu, 600, 0.125)
+    for a, b in zip((outs[0], lse, *grads), want):
+        assert torch.equal(a, b)
+    freqs, coords = binding.rope_frequencies(32).to(DEV), torch.arange(rows, dtype=torch.float32, device=DEV).reshape(-1, 1)
+    turned = torch.empty_like(q), torch.empty_like(k)
+    binding.ragged_rope(q, k, *turned, coords, freqs)
+    binding.ragged_rope(ins[0], ins[1], ins[0], ins[1], coords, freqs)
+    assert torch.equal(ins[0], turned[0]) and torch.equal(ins[1], turned[1])

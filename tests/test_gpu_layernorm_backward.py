@@ -147,3 +147,20 @@ def test_tensors_larger_than_the_caches(C, rows):
     _, _, wg, sg, wb, sb = _reference(x, gamma, dy, None, 1e-6)
     # (a column's values pass up to 500 additions here: 500 * 2^-24 = 3e-5 of the sum of sizes, and the error of xh)
     assert torch.all((dgamma.double() - wg).abs() <= 5e-5 * sg) and torch.all((dbeta.double() - wb).abs() <= 4e-5 * sb)
+
+
+def test_more_than_four_gigabytes():
+    """The last rows lie beyond 2^32 bytes; they are what they are in a call of their own."""
+    rows, C, last = 1060003, 2048, 1001
+    x = torch.zeros(rows, C, dtype=torch.bfloat16, device=DEV)
+    dy = torch.zeros_like(x)
+    x[-last:].normal_()
+    dy[-last:].normal_()
+    gamma, sums = torch.ones(C, dtype=torch.bfloat16, device=DEV), torch.empty(4, C, device=DEV)
+    workspace = torch.empty(binding.layernorm_backward_workspace(rows, C), dtype=torch.uint8, device=DEV)
+    want, dx = torch.empty_like(x[-last:]), torch.full_like(x, 7.0)
+    binding.ragged_layernorm_backward(x[-last:], gamma, dy[-last:], want, sums[0], sums[1], workspace)
+    binding.ragged_layernorm_backward(x, gamma, dy, dx, sums[2], sums[3], workspace)
+    assert torch.equal(dx[-last:], want) and not dx[:-last].any()
+    size = dy[-last:].double().abs().sum(0)
+    assert torch.all((sums[3].double() - sums[1].double()).abs() <= 2e-5 * size)      # (both off by 1e-5 of it at most)

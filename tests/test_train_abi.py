@@ -131,6 +131,17 @@ def test_grad_plan_covers_every_value_once(lib):
     assert at == chunks * size
 
 
+def test_grad_plan_of_a_tensor_beyond_32_bits(lib):
+    numel = (1 << 33) + 5
+    status, chunks = _plan(lib, [(FAKE, FAKE << 20, numel, 2, 2)])
+    assert status == 0
+    size = binding.GRAD_CHUNK_BYTES
+    table = ctypes.create_string_buffer(chunks * size)
+    assert _plan(lib, [(FAKE, FAKE << 20, numel, 2, 2)], ctypes.addressof(table), chunks * size) == (0, chunks)
+    s, d, n, *_ = struct.unpack_from("<QQiiii", table, (chunks - 1) * size)
+    assert s + 4 * n == FAKE + 4 * numel and d + 4 * n == (FAKE << 20) + 4 * numel
+
+
 def test_rope_frequencies(lib):
     for pairs, base in ((1, 10000.0), (10, 100.0), (32, 10000.0)):
         want = torch.tensor([base ** (-p / pairs) for p in range(pairs)], dtype=torch.float64)
