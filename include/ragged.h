@@ -364,6 +364,8 @@ int ragged_attn_lse(const void* q, const void* k, const void* v, void* o, float*
  * Supported: D = 64, dt = F16 or BF16; every token row on a 16-byte boundary; strides as for ragged_attn_strided (grad_tok_stride as
  * out_tok_stride).  max_seqlen <= 64 * 32767 and half of the work-groups of ragged_attn's limit.  Products on MFMA with fp32 sums;
  * P and dS are rounded to dt in between (with fp16, |dS| beyond 65504 overflows as the gradients themselves would).
+ * In sequences of up to 32 rows rowsum(dO * o) is formed as rowsum(P * dO v^T) in fp32 (the rounding of o does not tell), and a sequence of
+ * one row gets dq = dk = 0.
  * No atomics: results are bit-reproducible, and those of a sequence do not depend on the other sequences or on max_seqlen.
  */
 int ragged_attn_backward(const void* q, const void* k, const void* v, const void* o, const void* d_o, const float* lse, void* dq, void* dk,

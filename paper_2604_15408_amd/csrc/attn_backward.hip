@@ -3,8 +3,8 @@
 //     P_ij = exp(c q_i.k_j - L_i),   dP_ij = dO_i.v_j,   dS_ij = P_ij (dP_ij - delta_i),
 //     dV = P^T dO,   dK = c dS^T Q,   dQ = c dS K.
 //
-// One launch, no atomics, no workspace.  A sequence of at most 64 rows is one work-group's (whole_sequence: five products, dS turned
-// through LDS).  Of a longer one a work-group owns 128 rows (64 in small launches), either as KEYS, whose dK and dV it sums up over all query tiles, or as
+// One launch, no atomics, no workspace.  A sequence of at most 64 rows is one work-group's (whole_sequence, few_keys: five products, dS
+// turned through LDS).  Of a longer one a work-group owns 128 rows (64 in small launches), either as KEYS, whose dK and dV it sums up over all query tiles, or as
 // QUERIES, whose dQ it sums up over all key tiles (own_rows).  Both form P and dP again from 16-bit rows (seven products instead of the
 // five that a pass over both at once would need), which is what lets every sum have one owner and one order.
 //
@@ -311,21 +311,38 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
     }
 }
 
-// A whole sequence of at most 64 rows: P and dS are formed once, dS goes through LDS to the products that want it by queries.
+// Sum over the 16 lanes that share a row of scores (lanes 16 g .. 16 g + 15), in every one of them.
+template <int kCtrl>
+__device__ __forceinline__ float rotated(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float row_sum(float v) {
+    v += rotated<0x128>(v);                                    // row_ror:8
+    v += rotated<0x124>(v);
+    v += rotated<0x122>(v);
+    return v + rotated<0x121>(v);
+}
+
+// A whole sequence of at most kFewKeys rows: as whole_sequence, but delta is the sum over the keys of P dP in fp32, over the lanes of a
+// wavefront and then over the two that have keys; o is not read.  The same sum from the rounded o is off by u |dO| |o|, and the fewer the
+// keys the more that is beside the rounding of dS: with two keys dQ and dK were off by 3.3 thousandths in bf16, now by 2.4, as everywhere
+// above 40.  It costs a second round through LDS, us with o / with P dP: 32 x 12 tokens 4.4 / 4.6, 32 x 30 4.9 / 5.3, 256 x 30
+// 19.9 / 19.5; of all sequences up to 64 rows (four wavefronts, 64 queries each) 1 us of 6 to 12, hence the threshold.
+constexpr int kFewKeys = 32;
 template <typename In>
-__device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds, int s, int n, int h) {
+__device__ __forceinline__ void few_keys(const BackwardArgs& p, uint4* lds, int s, int n, int h) {
     typedef typename In::vec8 vec8;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int64_t head = (int64_t)h * kHeadDim;
     const float c2 = p.scale * kLog2e;
     const uint32_t q0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)lds);
-    const uint32_t do0 = q0 + kTileBytes, o0 = q0 + 2 * kTileBytes, k0 = q0 + 3 * kTileBytes, ds0 = q0 + 4 * kTileBytes;
-    const uint32_t lse0 = q0 + 2 * kSlotBytes;
-    float* const lse_lds = reinterpret_cast<float*>(lds) + 2 * kSlotBytes / 4;
-    f32x4* const stats = reinterpret_cast<f32x4*>(lse_lds + 2 * kBN);
-    const int blocks = (n + 31) >> 5;                          // of 32 rows: what the products touch
-    if (wave < 2 * blocks) {
+    const uint32_t do0 = q0 + kTileBytes, k0 = q0 + 2 * kTileBytes, ds0 = q0 + 3 * kTileBytes, lse0 = q0 + 4 * kTileBytes;
+    const f32x4* const lse_lds = reinterpret_cast<const f32x4*>(lds + 4 * kTileBytes / 16);
+    f32x4* const parts = reinterpret_cast<f32x4*>(lds + (4 * kTileBytes + kLseBytes) / 16);           // [wavefront][kFewKeys / 4]
+    static_assert(4 * kTileBytes + kLseBytes + 2 * kFewKeys * 4 <= kLdsBytes && kFewKeys == 32, "Q, dO, K, dS, L and the parts of delta");
+    const bool active = wave < 2;                              // 16 keys each, the second's may all be past the end (its part of dS is zeros)
+    if (active) {
         const uint32_t chunk = 16u * ((lane & 7) ^ ((lane >> 4) & 3));
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -335,7 +352,6 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
             const uint32_t at = wave * 2048 + i * 1024;
             dma16(q0 + at, in, p.q + (int64_t)s * p.in_tok + head);
             dma16(do0 + at, out, p.d_o + (int64_t)s * p.out_tok + head);
-            dma16(o0 + at, out, p.o + (int64_t)s * p.out_tok + head);
             dma16(k0 + at, in, p.k + (int64_t)s * p.in_tok + head);
         }
         if (wave == 0) dma4(lse0, (uint32_t)(lane < n ? lane : n - 1) * p.H * 4u, p.lse + (int64_t)s * p.H + h);
@@ -353,17 +369,119 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
     const uint32_t row_rel = col * 128 + 16 * ((2 * g) ^ ((col >> 1) & 3));
     const int tr_row = 4 * g + (col >> 2);
     const uint32_t tr_rel = tr_row * 128 + 16 * ((2 * (col & 3)) ^ ((tr_row >> 1) & 3));
+    auto transposed = [&](uint32_t tile, int dt) {
+        const uint32_t a = tile + (((dt & 2) ? tr_rel ^ 16u : tr_rel) + 8 * (dt & 1));
+        const uint2 lo = __builtin_bit_cast(uint2, lds_read_tr(a)), hi = __builtin_bit_cast(uint2, lds_read_tr(a + 16 * 128));
+        return as_vec8<vec8>(make_uint4(lo.x, lo.y, hi.x, hi.y));
+    };
     wait_vm<0>();
     __syncthreads();
-    const bool active = wave < 2 * blocks;                     // (a wavefront past the last key still fills its part of dS with zeros)
+    f32x4 pr[2], ds[2], part[2];                               // 16 queries each
     if (active) {
-        const uint32_t rb = do0 + row_rel + wave * 2048, ro = o0 + row_rel + wave * 2048;
-        const uint4 d[2] = {lds_read16(rb), lds_read16(rb ^ 16u)}, o[2] = {lds_read16(ro), lds_read16(ro ^ 16u)};
-        const float delta = diagonal<In>(d, o, col);
-        if (g == col >> 2) {
-            reinterpret_cast<float*>(stats)[own] = own < n ? lse_lds[own] * kLog2e : INFINITY;
-            reinterpret_cast<float*>(stats)[kBN + own] = own < n ? -delta : 0.f;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const uint32_t ra = q0 + row_rel + kt * 2048, rb = do0 + row_rel + kt * 2048;
+            pr[kt] = In::mfma(as_vec8<vec8>(lds_read16(ra)), kf[0], f32x4{0.f, 0.f, 0.f, 0.f});
+            ds[kt] = In::mfma(as_vec8<vec8>(lds_read16(rb)), vf[0], f32x4{0.f, 0.f, 0.f, 0.f});
+            pr[kt] = In::mfma(as_vec8<vec8>(lds_read16(ra ^ 16u)), kf[1], pr[kt]);
+            ds[kt] = In::mfma(as_vec8<vec8>(lds_read16(rb ^ 16u)), vf[1], ds[kt]);
+            const f32x4 row_lse = lse_lds[4 * kt + g];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(pr[kt][r], c2, -kLog2e * row_lse[r]));
+                const bool there = own < n && 16 * kt + 4 * g + r < n;
+                pr[kt][r] = there ? e : 0.f;
+                ds[kt][r] = there ? ds[kt][r] : 0.f;
+                part[kt][r] = row_sum(pr[kt][r] * ds[kt][r]);
+            }
+            if (col == 0) parts[wave * (kFewKeys / 4) + 4 * kt + g] = part[kt];
         }
+    }
+    __syncthreads();
+    if (active) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const f32x4 delta = parts[4 * kt + g] + parts[kFewKeys / 4 + 4 * kt + g];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) ds[kt][r] = n > 1 ? pr[kt][r] * (ds[kt][r] - delta[r]) : 0.f;  // (a single key has P = 1 whatever it is)
+        }
+        const vec8 p_op = operand(In{}, pr[0], pr[1]), ds_op = operand(In{}, ds[0], ds[1]);
+        // dS by keys: row own, queries 16 kt + 4 g .. + 3 in the same swizzled order as the other tiles
+        const uint4 w = __builtin_bit_cast(uint4, ds_op);
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const uint32_t at = ds0 + own * 128 + 16 * ((2 * kt + (g >> 1)) ^ ((own >> 1) & 3)) + 8 * (g & 1);
+            lds_write8(at, kt ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y));
+        }
+        f32x4 acc_k[4], acc_v[4];
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+            acc_k[dt] = In::mfma(transposed(q0, dt), ds_op, f32x4{0.f, 0.f, 0.f, 0.f});
+            acc_v[dt] = In::mfma(transposed(do0, dt), p_op, f32x4{0.f, 0.f, 0.f, 0.f});
+        }
+        if (own < n) {
+            const int64_t at = ((int64_t)s + own) * p.grad_tok + head + 16 * g;
+            store_row(In{}, p.dk + at, acc_k, p.scale);
+            store_row(In{}, p.dv + at, acc_v, 1.0f);
+        }
+    }
+    __syncthreads();
+    // dQ^T = K^T dS^T: in the transposed read this wavefront's columns are the queries 16 (col / 4) + 4 wave + col % 4
+    const int query = 16 * (col >> 2) + 4 * wave + (col & 3);
+    const vec8 ds_op = transposed(ds0, wave);
+    f32x4 acc_q[4];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) acc_q[dt] = In::mfma(transposed(k0, dt), ds_op, f32x4{0.f, 0.f, 0.f, 0.f});
+    if (query < n) store_row(In{}, p.dq + ((int64_t)s + query) * p.grad_tok + head + 16 * g, acc_q, p.scale);
+}
+
+// A whole sequence of 33 to 64 rows: P and dS are formed once, dS goes through LDS to the products that want it by queries.
+template <typename In>
+__device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds, int s, int n, int h) {
+    typedef typename In::vec8 vec8;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, g = lane >> 4;
+    const int64_t head = (int64_t)h * kHeadDim;
+    const float c2 = p.scale * kLog2e;
+    const uint32_t q0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)lds);
+    const uint32_t do0 = q0 + kTileBytes, o0 = q0 + 2 * kTileBytes, k0 = q0 + 3 * kTileBytes, ds0 = q0 + 4 * kTileBytes;
+    const uint32_t lse0 = q0 + 2 * kSlotBytes;
+    float* const lse_lds = reinterpret_cast<float*>(lds) + 2 * kSlotBytes / 4;
+    f32x4* const stats = reinterpret_cast<f32x4*>(lse_lds + 2 * kBN);
+    const uint32_t chunk = 16u * ((lane & 7) ^ ((lane >> 4) & 3));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        int rel = 16 * wave + 8 * i + (lane >> 3);
+        rel = rel < n ? rel : n - 1;                           // past the end: the last real row again
+        const uint32_t in = (uint32_t)rel * p.in_tok * 2u + chunk, out = (uint32_t)rel * p.out_tok * 2u + chunk;
+        const uint32_t at = wave * 2048 + i * 1024;
+        dma16(q0 + at, in, p.q + (int64_t)s * p.in_tok + head);
+        dma16(do0 + at, out, p.d_o + (int64_t)s * p.out_tok + head);
+        dma16(o0 + at, out, p.o + (int64_t)s * p.out_tok + head);
+        dma16(k0 + at, in, p.k + (int64_t)s * p.in_tok + head);
+    }
+    if (wave == 0) dma4(lse0, (uint32_t)(lane < n ? lane : n - 1) * p.H * 4u, p.lse + (int64_t)s * p.H + h);
+    // this lane's key: k and v, head-dim elements 16 g .. (zeros past the end)
+    const int own = 16 * wave + col;
+    uint4 own_k[2] = {}, own_v[2] = {};
+    if (own < n) {
+        const int64_t at = ((int64_t)s + own) * p.in_tok + head + 16 * g;
+        const uint4 *k = reinterpret_cast<const uint4*>(p.k + at), *v = reinterpret_cast<const uint4*>(p.v + at);
+        own_k[0] = k[0]; own_k[1] = k[1];
+        own_v[0] = v[0]; own_v[1] = v[1];
+    }
+    const vec8 kf[2] = {as_vec8<vec8>(own_k[0]), as_vec8<vec8>(own_k[1])}, vf[2] = {as_vec8<vec8>(own_v[0]), as_vec8<vec8>(own_v[1])};
+    const uint32_t row_rel = col * 128 + 16 * ((2 * g) ^ ((col >> 1) & 3));
+    const int tr_row = 4 * g + (col >> 2);
+    const uint32_t tr_rel = tr_row * 128 + 16 * ((2 * (col & 3)) ^ ((tr_row >> 1) & 3));
+    wait_vm<0>();
+    __syncthreads();
+    const uint32_t rb = do0 + row_rel + wave * 2048, ro = o0 + row_rel + wave * 2048;
+    const uint4 d[2] = {lds_read16(rb), lds_read16(rb ^ 16u)}, o[2] = {lds_read16(ro), lds_read16(ro ^ 16u)};
+    const float delta = diagonal<In>(d, o, col);
+    if (g == col >> 2) {
+        reinterpret_cast<float*>(stats)[own] = own < n ? lse_lds[own] * kLog2e : INFINITY;
+        reinterpret_cast<float*>(stats)[kBN + own] = own < n ? -delta : 0.f;
     }
     __syncthreads();
     f32x4 acc_k[4], acc_v[4];
@@ -374,45 +492,42 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
         const uint2 lo = __builtin_bit_cast(uint2, lds_read_tr(a)), hi = __builtin_bit_cast(uint2, lds_read_tr(a + 16 * 128));
         return as_vec8<vec8>(make_uint4(lo.x, lo.y, hi.x, hi.y));
     };
-    if (active) {
 #pragma unroll
-        for (int bb = 0; bb < 2; ++bb) {
-            if (bb >= blocks) break;
-            f32x4 pr[2], ds[2];
+    for (int bb = 0; bb < 2; ++bb) {
+        f32x4 pr[2], ds[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int kt = 2 * bb + u;
-                const uint32_t ra = q0 + row_rel + kt * 2048, rb = do0 + row_rel + kt * 2048;
-                const f32x4 row_lse = stats[4 * kt + g];
-                pr[u] = In::mfma(as_vec8<vec8>(lds_read16(ra)), kf[0], f32x4{0.f, 0.f, 0.f, 0.f});
-                ds[u] = In::mfma(as_vec8<vec8>(lds_read16(rb)), vf[0], stats[kBN / 4 + 4 * kt + g]);
-                pr[u] = In::mfma(as_vec8<vec8>(lds_read16(ra ^ 16u)), kf[1], pr[u]);
-                ds[u] = In::mfma(as_vec8<vec8>(lds_read16(rb ^ 16u)), vf[1], ds[u]);
+        for (int u = 0; u < 2; ++u) {
+            const int kt = 2 * bb + u;
+            const uint32_t ra = q0 + row_rel + kt * 2048, rb = do0 + row_rel + kt * 2048;
+            const f32x4 row_lse = stats[4 * kt + g];
+            pr[u] = In::mfma(as_vec8<vec8>(lds_read16(ra)), kf[0], f32x4{0.f, 0.f, 0.f, 0.f});
+            ds[u] = In::mfma(as_vec8<vec8>(lds_read16(rb)), vf[0], stats[kBN / 4 + 4 * kt + g]);
+            pr[u] = In::mfma(as_vec8<vec8>(lds_read16(ra ^ 16u)), kf[1], pr[u]);
+            ds[u] = In::mfma(as_vec8<vec8>(lds_read16(rb ^ 16u)), vf[1], ds[u]);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    pr[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(pr[u][r], c2, -row_lse[r]));
-                    ds[u][r] = own < n ? pr[u][r] * ds[u][r] : 0.f;
-                }
-            }
-            const vec8 p_op = operand(In{}, pr[0], pr[1]), ds_op = operand(In{}, ds[0], ds[1]);
-            // dS by keys: row own, queries 16 kt + 4 g .. + 3 in the same swizzled order as the other tiles
-            const uint4 w = __builtin_bit_cast(uint4, ds_op);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint32_t at = ds0 + own * 128 + 16 * ((2 * (2 * bb + u) + (g >> 1)) ^ ((own >> 1) & 3)) + 8 * (g & 1);
-                lds_write8(at, u ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y));
-            }
-#pragma unroll
-            for (int dt = 0; dt < 4; ++dt) {
-                acc_k[dt] = In::mfma(transposed(q0, dt, bb), ds_op, acc_k[dt]);
-                acc_v[dt] = In::mfma(transposed(do0, dt, bb), p_op, acc_v[dt]);
+            for (int r = 0; r < 4; ++r) {
+                pr[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(pr[u][r], c2, -row_lse[r]));
+                ds[u][r] = own < n ? pr[u][r] * ds[u][r] : 0.f;
             }
         }
-        if (own < n) {
-            const int64_t at = ((int64_t)s + own) * p.grad_tok + head + 16 * g;
-            store_row(In{}, p.dk + at, acc_k, p.scale);
-            store_row(In{}, p.dv + at, acc_v, 1.0f);
+        const vec8 p_op = operand(In{}, pr[0], pr[1]), ds_op = operand(In{}, ds[0], ds[1]);
+        // dS by keys: row own, queries 16 kt + 4 g .. + 3 in the same swizzled order as the other tiles
+        const uint4 w = __builtin_bit_cast(uint4, ds_op);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t at = ds0 + own * 128 + 16 * ((2 * (2 * bb + u) + (g >> 1)) ^ ((own >> 1) & 3)) + 8 * (g & 1);
+            lds_write8(at, u ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y));
         }
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+            acc_k[dt] = In::mfma(transposed(q0, dt, bb), ds_op, acc_k[dt]);
+            acc_v[dt] = In::mfma(transposed(do0, dt, bb), p_op, acc_v[dt]);
+        }
+    }
+    if (own < n) {
+        const int64_t at = ((int64_t)s + own) * p.grad_tok + head + 16 * g;
+        store_row(In{}, p.dk + at, acc_k, p.scale);
+        store_row(In{}, p.dv + at, acc_v, 1.0f);
     }
     __syncthreads();
     // dQ^T += K^T dS^T: in the transposed read this wavefront's columns are the queries 16 (col / 4) + 4 wave + col % 4
@@ -422,7 +537,6 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
     for (int dt = 0; dt < 4; ++dt) acc_q[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int bb = 0; bb < 2; ++bb) {
-        if (bb >= blocks) break;
         const vec8 ds_op = transposed(ds0, wave, bb);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) acc_q[dt] = In::mfma(transposed(k0, dt, bb), ds_op, acc_q[dt]);
@@ -444,7 +558,10 @@ void attn_backward_kernel(const int32_t* __restrict__ cu_seqlens, int H, uint32_
     const int m0 = tile * 64 * CB;
     if (m0 >= n) return;
     if (__builtin_expect(n <= kBN, 1)) {
-        if (y == 0) whole_sequence<In>(p, lds, s, n, (int)h);
+        if (y == 0) {
+            if (n <= kFewKeys) few_keys<In>(p, lds, s, n, (int)h);
+            else whole_sequence<In>(p, lds, s, n, (int)h);
+        }
         return;
     }
     if (y != tile) own_rows<In, false, CB>(p, lds, s, n, (int)h, m0);

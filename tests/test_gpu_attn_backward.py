@@ -103,6 +103,35 @@ def test_gradients(lengths, dtype):
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_few_keys(dtype):
+    """Up to 32 keys delta is sum P dP in fp32 and carries no rounding of o: each dP is off by 2^-18 sum|dO v| and each P by e of itself, their
+    sum over 32 keys by 2^-21 more.  One key has P = 1 whatever q and k are: dq and dk are zeros."""
+    lengths, scale = [1, 2, 3, 1, 15, 16, 17, 31, 32, 8], 0.125
+    rows, q, k, v, do, cu = _inputs(lengths, 3, dtype, 21)
+    do[:rows] = do[:rows] * 0.1 + 1.0                          # delta well beside dP, as where the rounding of o would tell
+    o, lse, dq, dk, dv = _run(q, k, v, do, cu, 32, scale)
+    u, tiny = torch.finfo(q.dtype).eps / 2, 2.0 ** -25 if dtype == "f16" else 0.0
+    ends = cu.tolist()
+    for lo, hi in zip(ends[:-1], ends[1:]):
+        if hi - lo == 1:
+            assert torch.all(dq[lo] == 0) and torch.all(dk[lo] == 0) and torch.equal(dv[lo], do[lo])
+            continue
+        Q, K, V, dO = (t[lo:hi].cpu().double().transpose(0, 1) for t in (q, k, v, do))
+        T = lambda t: t.transpose(1, 2)
+        S = scale * (Q @ T(K))
+        L = torch.logsumexp(S, dim=-1)
+        P, dP = torch.exp(S - L[..., None]), dO @ T(V)
+        dS = P * (dP - (P * dP).sum(-1, keepdim=True))
+        e = 2.0 ** -18 * (scale * (Q.abs() @ T(K.abs()))).amax(dim=-1, keepdim=True) + 2.0 ** -22 * (4 + L.abs()[..., None])
+        off = 2.0 ** -18 * (dO.abs() @ T(V.abs()))
+        delta_off = (P * (dP.abs() * (e + 2.0 ** -21) + off)).sum(-1, keepdim=True)
+        b = dS.abs() * (u + e) + P * (off + delta_off) + (P * dP).abs() * 2.0 ** -22 + tiny
+        for got, want, bound in ((dq, scale * (dS @ K), scale * (b @ K.abs())), (dk, scale * (T(dS) @ Q), scale * (T(b) @ Q.abs()))):
+            err = (got[lo:hi].cpu().double().transpose(0, 1) - want).abs()
+            assert torch.all(err <= bound + u * want.abs() + tiny), (lo, hi, float((err - bound).max()))
+
+
 @pytest.mark.parametrize("scale", [-0.25, 0.0, 1.0])
 def test_scales(scale):
     rows, q, k, v, do, cu = _inputs([70, 20], 2, "f16", 11)
