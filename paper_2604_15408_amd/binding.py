@@ -628,7 +628,6 @@ class GradPlan:
         self.workspace = torch.empty(GRAD_WORKSPACE, dtype=torch.uint8, device=grads[0].device)
         self.tensors = (grads, outs)
 
-
     @staticmethod
     def _refuse_overlaps(grads, outs):
         """No output may lie over another one or over a gradient that is not its own (all of it): they are read and written in any order."""

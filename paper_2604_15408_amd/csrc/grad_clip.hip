@@ -210,8 +210,9 @@ hipError_t launch_grad_clip(const void* table, int chunks, float scale, float ma
     const int groups = chunks < 1 ? 1 : chunks < kClipGroups ? chunks : kClipGroups;
     const hipError_t err = launch_kernel(grad_squares_kernel, dim3(groups), dim3(kBlockThreads), stream, t, chunks, partial);
     if (err != hipSuccess) return err;
-    return launch_kernel((int64_t)chunks * kChunk > kClipBypass ? grad_scale_kernel<true> : grad_scale_kernel<false>, dim3(groups), dim3(kBlockThreads), stream, t, chunks, static_cast<const double*>(partial), groups,
-                         scale, max_norm, norm);
+    const auto kernel = (int64_t)chunks * kChunk > kClipBypass ? grad_scale_kernel<true> : grad_scale_kernel<false>;
+    return launch_kernel(kernel, dim3(groups), dim3(kBlockThreads), stream, t, chunks, static_cast<const double*>(partial), groups, scale, max_norm,
+                         norm);
 }
 
 }  // namespace ragged
