@@ -24,12 +24,23 @@
 // P and dS are rounded to the input type for the second products, as the gradients themselves are in the end: a sum of n terms
 // whose signs are mixed is off by about as much as its own rounding.  Sums are fp32.
 //
+// fp16 has the bits for that and not the range: P = 1/n is below its normal numbers beyond 16 384 keys, dS overflows at 65 504 where dQ and dK
+// need not, and vanishes where gradients are small.  So P is rounded as 2^15 P, and dS as F dS; both are taken out of the fp32 sums.
+// |dS| <= |dP - delta| <= 2 |dO| |v|, and F is the power of two with which 2 |dO| |v| is below 2^14, |dO| and |v| being the lengths of several
+// rows as one vector.  Up to 64 rows that is all of them.  Of a longer sequence it is 4 rows, spread evenly over it, so that F is the same in every
+// work-group and launch (past queries a query's own dO): with N(0, 1) rows F = 16 and |F (dP - delta)| is up to 2^9.  Where far larger rows come
+// all the same, the sums of a column end as infinities or no numbers, all of them: such columns are gone through again with 2^-16 F, down to
+// 2^-24, with which no dS overflows; the others have been stored.  F is in the exponent that P is formed with, so that the loop has one
+// multiplication more past keys (from F P to 2^15 P), and none past queries.  Launches of fp16 take 2 to 8 % more for it, most of it for the
+// sample (64 x 128 28.5 -> 30.4 us, 128 x about 100 38.2 -> 41.1, 64 x 197 55.6 -> 58, 32 x 577 144 -> 149, 256 x 30 19.4 -> 20.4).
+//
 // us now (gradients alone, H = 12): 32 x 577 bf16 141 (82 GFLOP in five products, 115 in the seven of this form: 0.8 PFLOP/s, where a loop of
 // products alone sustains 1.3), 64 x 197 fp16 52 (155 MB of rows: 26 us at the rate of a copy), 32 x about 40 bf16 6.7.
 #include <type_traits>
 
 #include "attn_parts.h"
 #include "common.h"
+#include "lane_sums.h"
 #include "mfma_lds.h"
 
 namespace ragged {
@@ -49,7 +60,8 @@ constexpr int64_t kGroupBytes = 3 << 20;
 constexpr int kAtOnce = 2048;
 constexpr int kSlotBytes = 3 * kTileBytes;      // tiles A and B; keys: the rows of o besides
 constexpr int kLseBytes = kBN * 4;
-constexpr int kLdsBytes = 2 * kSlotBytes + 2 * kLseBytes + 2 * kBN * 4;      // ring, L of a tile's queries, statistics (L log2 e, - delta)
+constexpr int kVotes = 2 * kSlotBytes + 2 * kLseBytes + 2 * kBN * 4;         // ring, L of a tile's queries, statistics (L log2 e, - delta) and
+constexpr int kLdsBytes = kVotes + kBlockThreads / kWaveSize * 8;            // a word or two of each wavefront
 
 struct BackwardArgs {
     const uint16_t *q, *k, *v, *o, *d_o;
@@ -97,6 +109,28 @@ __device__ __forceinline__ bf16x8 operand(BF16, const f32x4& lo, const f32x4& hi
     return v;
 }
 
+// fp16's powers of two: 2^kFitP for P, 2^fit for dS, fit from squares of the lengths of what dO and v are to be sized by (0: nothing to go by, 1).
+template <typename In> constexpr bool kFit = std::is_same<In, F16>::value;
+constexpr int kFitP = 15, kFitLast = -24, kFitStep = 16, kFitMost = 60;
+__device__ __forceinline__ float power2(int e) { return __builtin_bit_cast(float, (uint32_t)(127 + e) << 23); }
+__device__ __forceinline__ int exponent(float v) { return (int)(__builtin_bit_cast(uint32_t, v) >> 23 & 255) - 127; }
+__device__ __forceinline__ int fit_within(int fit) { return fit < kFitLast ? kFitLast : fit > kFitMost ? kFitMost : fit; }
+__device__ __forceinline__ int fit_of(float squares_do, float squares_v) {
+    const float a = squares_do == 0.f ? 1.f : squares_do, b = squares_v == 0.f ? 1.f : squares_v;
+    return fit_within(12 - (exponent(a * b) >> 1));            // 2 sqrt(a b) < 2^(exponent / 2 + 2)
+}
+__device__ __forceinline__ float squares(const uint4& w) {
+    const f16x8 v = as_vec8<f16x8>(w);
+    float even = 0.f, odd = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        even = __builtin_fmaf((float)v[e], (float)v[e], even);
+        odd = __builtin_fmaf((float)v[e + 1], (float)v[e + 1], odd);
+    }
+    return even + odd;
+}
+
+// A lane's 16 sums, times the scale (and what they were formed with taken out), as elements of a row.
 __device__ __forceinline__ void store_row(F16, uint16_t* dst, const f32x4 (&acc)[4], float times) {
     float v[16];
 #pragma unroll
@@ -132,12 +166,12 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
     const uint32_t lse0 = ring0 + 2 * kSlotBytes;
     float* const lse_lds = reinterpret_cast<float*>(lds) + 2 * kSlotBytes / 4;
     f32x4* const stats = reinterpret_cast<f32x4*>(lse_lds + 2 * kBN);         // [2][kBN / 4]
+    uint32_t* const votes = reinterpret_cast<uint32_t*>(lds) + kVotes / 4;
     const uint16_t* const base_o = p.o + (int64_t)s * tok_b + head;           // (keys)
     const int tiles = (n + kBN - 1) / kBN;
     const int load_row = 16 * wave + (lane >> 3);
     const uint32_t load_chunk = 16u * ((lane & 7) ^ ((lane >> 4) & 3));
-    auto issue = [&](int t, int slot) {
-        const int rem = n - t * kBN;
+    auto issue = [&](int t, int slot, int rem) {
         const int need = rem >= kBN ? kBN : 32 * ((rem + 31) >> 5);       // rows the tile's products touch
         if (16 * wave >= need) return;
         const uint32_t dst = ring0 + slot * kSlotBytes + wave * 2048;
@@ -152,33 +186,60 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
         if (KEYS && wave == 0)
             dma4(lse0 + slot * kLseBytes, (uint32_t)(lane < rem ? lane : rem - 1) * p.H * 4u, p.lse + ((int64_t)s + t * kBN) * p.H + h);
     };
-    issue(0, 0);
+    issue(0, 0, n);
 
     // ---- this lane's columns: two operands, 16 head-dim elements (16 g ..) of each (zeros past the end)
     vec8 col_a[CB][2], col_b[CB][2];                           // k, v or q, dO
     float lse2[CB], minus_delta[CB];                           // queries: statistics of the columns
+    int fit[CB];                                               // fp16; keys: one for the sequence, queries: one for each column
+    bool todo[CB];                                             // columns that are there and not stored yet
+    uint4 own_a[CB][2] = {}, own_b[CB][2] = {}, own_o[CB][2] = {};
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
-        uint4 own_a[2] = {}, own_b[2] = {}, own_o[2] = {};
-        lse2[cb] = minus_delta[cb] = 0.f;
+        lse2[cb] = 0.f;
         const int own = first + 16 * cb + col;
+        todo[cb] = own < n;
         if (own < n) {
             const int64_t row = (int64_t)s + own;
             const uint4* a = reinterpret_cast<const uint4*>((KEYS ? p.k : p.q) + row * p.in_tok + head + 16 * g);
             const uint4* b = reinterpret_cast<const uint4*>(KEYS ? p.v + row * p.in_tok + head + 16 * g : p.d_o + row * p.out_tok + head + 16 * g);
-            own_a[0] = a[0]; own_a[1] = a[1];
-            own_b[0] = b[0]; own_b[1] = b[1];
+            own_a[cb][0] = a[0]; own_a[cb][1] = a[1];
+            own_b[cb][0] = b[0]; own_b[cb][1] = b[1];
             if (!KEYS) {
                 const uint4* o = reinterpret_cast<const uint4*>(p.o + row * p.out_tok + head + 16 * g);
-                own_o[0] = o[0]; own_o[1] = o[1];
-                lse2[cb] = p.lse[row * p.H + h] * kLog2e;
+                own_o[cb][0] = o[0]; own_o[cb][1] = o[1];
+                lse2[cb] = p.lse[row * p.H + h];
             }
         }
-        if (!KEYS) minus_delta[cb] = -__shfl(diagonal<In>(own_b, own_o, col), 16 * (col >> 2) + col);
+    }
+    // fp16: squares of 4 rows of the sequence, from the first to the last: v by 8 lanes each, dO by the other 32
+    float size_v = 0.f, size_do = 0.f;
+    if constexpr (kFit<In>) {
+        uint4 sample = {};
+        if (KEYS || lane < 32) {
+            const int64_t row = (int64_t)s + (lane >> 3 & 3) * (n - 1) / 3, at = head + 8 * (lane & 7);
+            sample = *reinterpret_cast<const uint4*>(lane < 32 ? p.v + row * p.in_tok + at : p.d_o + row * p.out_tok + at);
+        }
+        const float sum = lanes_sum_f32<32>(squares(sample));
+        size_v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sum), 0));
+        size_do = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sum), 32));
+    }
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        minus_delta[cb] = 0.f;
+        lse2[cb] *= kLog2e;
+        if (!KEYS) minus_delta[cb] = -__shfl(diagonal<In>(own_b[cb], own_o[cb], col), 16 * (col >> 2) + col);
+        fit[cb] = 0;
+        if constexpr (kFit<In>) {
+            // (4 times the square of a query's own row: what 4 such rows would have in the sample)
+            fit[cb] = KEYS ? fit_of(size_do, size_v)
+                           : fit_of(4.f * quad_sum(squares(own_b[cb][0]) + squares(own_b[cb][1])), size_v);
+            if (!KEYS) lse2[cb] -= (float)fit[cb];
+        }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            col_a[cb][ks] = as_vec8<vec8>(own_a[ks]);
-            col_b[cb][ks] = as_vec8<vec8>(own_b[ks]);
+            col_a[cb][ks] = as_vec8<vec8>(own_a[cb][ks]);
+            col_b[cb][ks] = as_vec8<vec8>(own_b[cb][ks]);
         }
     }
 
@@ -196,10 +257,7 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
         asm volatile("" : "+v"(lse2[cb]), "+v"(minus_delta[cb]));
     }
     f32x4 acc_a[CB][4], acc_b[CB][4];                          // dK^T or dQ^T; dV^T
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt) acc_a[cb][dt] = acc_b[cb][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float p_times = 1.f;                                       // fp16, keys: from F P to 2^15 P
 
     // keys: the statistics of a tile's queries, 16 of them by each wavefront; behind the last query exp2(.. - inf) = 0
     auto write_stats = [&](int t, int slot) {
@@ -208,7 +266,8 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
         const float delta = diagonal<In>(d, o, col);
         if (g == col >> 2) {
             const bool there = t * kBN + 16 * wave + col < n;
-            reinterpret_cast<float*>(stats)[16 * wave + col] = there ? lse_lds[slot * kBN + 16 * wave + col] * kLog2e : INFINITY;
+            const float own_lse = lse_lds[slot * kBN + 16 * wave + col] * kLog2e;
+            reinterpret_cast<float*>(stats)[16 * wave + col] = there ? kFit<In> ? own_lse - (float)fit[0] : own_lse : INFINITY;
             reinterpret_cast<float*>(stats)[kBN + 16 * wave + col] = there ? -delta : 0.f;
         }
     };
@@ -217,7 +276,7 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
     auto block = [&](uint32_t tile, int bb, int rem, auto mask, auto subtiles) {
         constexpr bool MASK = decltype(mask)::value;
         constexpr int NU = decltype(subtiles)::value;
-        f32x4 pr[CB][2], ds[CB][2];
+        f32x4 pr[CB][2], ds[CB][2];                            // P and dS (fp16: 2^15 P, F dS)
         if (NU == 1) {
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) pr[cb][1] = ds[cb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -245,6 +304,11 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
                     float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], c2, KEYS ? -row_lse[r] : -lse2[cb]));
                     if (MASK && !KEYS) e = 16 * kt + 4 * g + r < rem ? e : 0.f;
                     pr[cb][u][r] = e;
+                    if (kFit<In> && KEYS) {                    // (kept apart from its conversion: one fma and conversion each takes longer)
+                        float scaled = e * p_times;
+                        asm("" : "+v"(scaled));
+                        pr[cb][u][r] = scaled;
+                    }
                     ds[cb][u][r] = e * dp[r];
                 }
             }
@@ -271,43 +335,73 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
             }
         }
     };
-    for (int t = 0; t < tiles; ++t) {
-        const int slot = t & 1;
-        wait_vm<0>();
-        __syncthreads();                                       // tile t is there; everyone is past the reads of tile t - 1
-        if (t + 1 < tiles) issue(t + 1, slot ^ 1);
-        if (KEYS) {
-            if (t * kBN + 16 * wave < n + 16) write_stats(t, slot);
-            __syncthreads();
-        }
-        if (active) {
-            const uint32_t tile = ring0 + slot * kSlotBytes;
-            const int rem = n - t * kBN;
-            typedef std::integral_constant<int, 1> Half;
-            typedef std::integral_constant<int, 2> Whole;
-            // a last block of at most 16 rows has a form of its own: 64 x 197 tokens 57.4 -> 54.7 us (CB = 1, a chain of latencies, gains nothing)
-            const int whole = rem >= kBN ? 2 : CB == 1 ? (rem + 31) >> 5 : (rem + 15) >> 5;
-            if (KEYS || rem >= kBN) {
-#pragma nounroll
-                for (int bb = 0; bb < whole; ++bb) block(tile, bb, rem, std::false_type{}, Whole{});
-            } else {
-#pragma nounroll
-                for (int bb = 0; bb < whole; ++bb) block(tile, bb, rem, std::true_type{}, Whole{});
-            }
-            if constexpr (CB > 1) {
-                if (32 * whole < rem && rem < kBN) block(tile, whole, rem, std::true_type{}, Half{});
-            }
-        }
-    }
-    // this lane owns elements 16 g .. 16 g + 15 of its rows
+    for (;;) {
+        float zero = 0.f;
+        if (kFit<In>) asm volatile("v_mov_b32 %0, 0" : "=v"(zero));                          // (made here, not kept in four registers)
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        const int own = first + 16 * cb + col;
-        if (own < n) {
-            const int64_t at = ((int64_t)s + own) * p.grad_tok + head + 16 * g;
-            store_row(In{}, (KEYS ? p.dk : p.dq) + at, acc_a[cb], p.scale);
-            if (KEYS) store_row(In{}, p.dv + at, acc_b[cb], 1.0f);
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) acc_a[cb][dt] = acc_b[cb][dt] = f32x4{zero, zero, zero, zero};
+        if (kFit<In> && KEYS) p_times = power2(kFitP - fit[0]);
+        for (int t = 0; t < tiles; ++t) {
+            const int slot = t & 1;
+            wait_vm<0>();
+            __syncthreads();                                       // tile t is there; everyone is past the reads of tile t - 1
+            if (t + 1 < tiles) issue(t + 1, slot ^ 1, n - (t + 1) * kBN);
+            if (KEYS) {
+                if (t * kBN + 16 * wave < n + 16) write_stats(t, slot);
+                __syncthreads();
+            }
+            if (active) {
+                const uint32_t tile = ring0 + slot * kSlotBytes;
+                const int rem = n - t * kBN;
+                typedef std::integral_constant<int, 1> Half;
+                typedef std::integral_constant<int, 2> Whole;
+                // a last block of at most 16 rows has a form of its own: 64 x 197 tokens 57.4 -> 54.7 us (CB = 1, a chain of latencies, gains nothing)
+                const int whole = rem >= kBN ? 2 : CB == 1 ? (rem + 31) >> 5 : (rem + 15) >> 5;
+                if (KEYS || rem >= kBN) {
+#pragma nounroll
+                    for (int bb = 0; bb < whole; ++bb) block(tile, bb, rem, std::false_type{}, Whole{});
+                } else {
+#pragma nounroll
+                    for (int bb = 0; bb < whole; ++bb) block(tile, bb, rem, std::true_type{}, Whole{});
+                }
+                if constexpr (CB > 1) {
+                    if (32 * whole < rem && rem < kBN) block(tile, whole, rem, std::true_type{}, Half{});
+                }
+            }
         }
+        // this lane owns elements 16 g .. 16 g + 15 of its rows
+        bool left = false;
+        int here = lane;
+        asm volatile("" : "+v"(here));                             // (addresses formed here, not kept through the loop)
+        const int64_t lane_at = ((int64_t)s + (first + (here & 15))) * p.grad_tok + head + 16 * (here >> 4);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            if (!todo[cb]) continue;
+            if (kFit<In> && fit[cb] > kFitLast && !(fabsf(acc_a[cb][0][0]) < INFINITY)) {
+                left = true;                                       // (the same in the four lanes of the column)
+                continue;
+            }
+            todo[cb] = false;
+            const int64_t at = lane_at + (int64_t)(16 * cb) * p.grad_tok;
+            store_row(In{}, (KEYS ? p.dk : p.dq) + at, acc_a[cb], p.scale * power2(-fit[cb]));
+            if (KEYS) store_row(In{}, p.dv + at, acc_b[cb], kFit<In> ? power2(-kFitP) : 1.0f);
+        }
+        if (!kFit<In>) return;
+        const uint64_t any = __ballot(left);
+        if (lane == 0) votes[wave] = any != 0;
+        __syncthreads();                                           // everyone is past the last tile, too
+        if ((votes[0] | votes[1] | votes[2] | votes[3]) == 0) return;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {                          // (past queries the columns that are done are only gone through)
+            const int lower = fit_within(fit[cb] - kFitStep);
+            if (!KEYS) lse2[cb] += (float)(fit[cb] - lower);
+            fit[cb] = lower;
+        }
+        int rows = n;
+        asm volatile("" : "+s"(rows));                             // (nor these)
+        issue(0, 0, rows);
     }
 }
 
@@ -340,7 +434,8 @@ __device__ __forceinline__ void few_keys(const BackwardArgs& p, uint4* lds, int 
     const uint32_t do0 = q0 + kTileBytes, k0 = q0 + 2 * kTileBytes, ds0 = q0 + 3 * kTileBytes, lse0 = q0 + 4 * kTileBytes;
     const f32x4* const lse_lds = reinterpret_cast<const f32x4*>(lds + 4 * kTileBytes / 16);
     f32x4* const parts = reinterpret_cast<f32x4*>(lds + (4 * kTileBytes + kLseBytes) / 16);           // [wavefront][kFewKeys / 4]
-    static_assert(4 * kTileBytes + kLseBytes + 2 * kFewKeys * 4 <= kLdsBytes && kFewKeys == 32, "Q, dO, K, dS, L and the parts of delta");
+    uint32_t* const votes = reinterpret_cast<uint32_t*>(lds) + kVotes / 4;
+    static_assert(4 * kTileBytes + kLseBytes + 2 * kFewKeys * 4 <= kVotes && kFewKeys == 32, "Q, dO, K, dS, L and the parts of delta");
     const bool active = wave < 2;                              // 16 keys each, the second's may all be past the end (its part of dS is zeros)
     if (active) {
         const uint32_t chunk = 16u * ((lane & 7) ^ ((lane >> 4) & 3));
@@ -388,7 +483,7 @@ __device__ __forceinline__ void few_keys(const BackwardArgs& p, uint4* lds, int 
             const f32x4 row_lse = lse_lds[4 * kt + g];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(pr[kt][r], c2, -kLog2e * row_lse[r]));
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(pr[kt][r], c2, __builtin_fmaf(-kLog2e, row_lse[r], kFit<In> ? kFitP : 0)));
                 const bool there = own < n && 16 * kt + 4 * g + r < n;
                 pr[kt][r] = there ? e : 0.f;
                 ds[kt][r] = there ? ds[kt][r] : 0.f;
@@ -396,14 +491,32 @@ __device__ __forceinline__ void few_keys(const BackwardArgs& p, uint4* lds, int 
             }
             if (col == 0) parts[wave * (kFewKeys / 4) + 4 * kt + g] = part[kt];
         }
+        if constexpr (kFit<In>) {                              // the largest |dP|; delta is no larger
+            float most = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(ds[e / 4][e % 4]));
+            most = fmaxf(most, rotated<0x128>(most));
+            most = fmaxf(most, rotated<0x124>(most));
+            most = fmaxf(most, rotated<0x122>(most));
+            most = quad_max(fmaxf(most, rotated<0x121>(most)));
+            if (lane == 0) votes[wave] = as_u32(most);
+        }
     }
     __syncthreads();
+    int fit = 0;
+    if constexpr (kFit<In>) {
+        const float most = fmaxf(as_f32(votes[0]), as_f32(votes[1]));
+        fit = fit_within(most == 0.f ? 0 : 13 - exponent(most));                         // |dP - delta| < 2^(exponent + 2)
+    }
     if (active) {
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             const f32x4 delta = parts[4 * kt + g] + parts[kFewKeys / 4 + 4 * kt + g];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) ds[kt][r] = n > 1 ? pr[kt][r] * (ds[kt][r] - delta[r]) : 0.f;  // (a single key has P = 1 whatever it is)
+            for (int r = 0; r < 4; ++r) {                      // fp16: delta and P come with 2^kFitP
+                const float from = kFit<In> ? __builtin_fmaf(ds[kt][r], power2(fit - kFitP), -power2(fit - 2 * kFitP) * delta[r]) : ds[kt][r] - delta[r];
+                ds[kt][r] = n > 1 ? pr[kt][r] * from : 0.f;    // (a single key has P = 1 whatever it is)
+            }
         }
         const vec8 p_op = operand(In{}, pr[0], pr[1]), ds_op = operand(In{}, ds[0], ds[1]);
         // dS by keys: row own, queries 16 kt + 4 g .. + 3 in the same swizzled order as the other tiles
@@ -421,8 +534,8 @@ __device__ __forceinline__ void few_keys(const BackwardArgs& p, uint4* lds, int 
         }
         if (own < n) {
             const int64_t at = ((int64_t)s + own) * p.grad_tok + head + 16 * g;
-            store_row(In{}, p.dk + at, acc_k, p.scale);
-            store_row(In{}, p.dv + at, acc_v, 1.0f);
+            store_row(In{}, p.dk + at, acc_k, p.scale * power2(-fit));
+            store_row(In{}, p.dv + at, acc_v, kFit<In> ? power2(-kFitP) : 1.0f);
         }
     }
     __syncthreads();
@@ -432,7 +545,7 @@ __device__ __forceinline__ void few_keys(const BackwardArgs& p, uint4* lds, int 
     f32x4 acc_q[4];
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) acc_q[dt] = In::mfma(transposed(k0, dt), ds_op, f32x4{0.f, 0.f, 0.f, 0.f});
-    if (query < n) store_row(In{}, p.dq + ((int64_t)s + query) * p.grad_tok + head + 16 * g, acc_q, p.scale);
+    if (query < n) store_row(In{}, p.dq + ((int64_t)s + query) * p.grad_tok + head + 16 * g, acc_q, p.scale * power2(-fit));
 }
 
 // A whole sequence of 33 to 64 rows: P and dS are formed once, dS goes through LDS to the products that want it by queries.
@@ -448,6 +561,7 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
     const uint32_t lse0 = q0 + 2 * kSlotBytes;
     float* const lse_lds = reinterpret_cast<float*>(lds) + 2 * kSlotBytes / 4;
     f32x4* const stats = reinterpret_cast<f32x4*>(lse_lds + 2 * kBN);
+    float* const sums = reinterpret_cast<float*>(lds) + kVotes / 4;                     // [2][wavefront]
     const uint32_t chunk = 16u * ((lane & 7) ^ ((lane >> 4) & 3));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -480,10 +594,21 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
     const uint4 d[2] = {lds_read16(rb), lds_read16(rb ^ 16u)}, o[2] = {lds_read16(ro), lds_read16(ro ^ 16u)};
     const float delta = diagonal<In>(d, o, col);
     if (g == col >> 2) {
-        reinterpret_cast<float*>(stats)[own] = own < n ? lse_lds[own] * kLog2e : INFINITY;
+        reinterpret_cast<float*>(stats)[own] = own < n ? __builtin_fmaf(lse_lds[own], kLog2e, kFit<In> ? -kFitP : 0) : INFINITY;
         reinterpret_cast<float*>(stats)[kBN + own] = own < n ? -delta : 0.f;
     }
+    if constexpr (kFit<In>) {                                  // of all rows of dO (the last one again past the end) and of v
+        const float of_do = lanes_sum_f32<kWaveSize>(squares(d[0]) + squares(d[1])),
+                    of_v = lanes_sum_f32<kWaveSize>(squares(own_v[0]) + squares(own_v[1]));
+        if (lane == 0) {
+            sums[wave] = of_do;
+            sums[4 + wave] = of_v;
+        }
+    }
     __syncthreads();
+    int fit = 0;
+    if constexpr (kFit<In>)
+        fit = fit_of((sums[0] + sums[1]) + (sums[2] + sums[3]), (sums[4] + sums[5]) + (sums[6] + sums[7]));
     f32x4 acc_k[4], acc_v[4];
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) acc_k[dt] = acc_v[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -507,7 +632,8 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 pr[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(pr[u][r], c2, -row_lse[r]));
-                ds[u][r] = own < n ? pr[u][r] * ds[u][r] : 0.f;
+                const float e = kFit<In> ? pr[u][r] * power2(fit - kFitP) : pr[u][r];
+                ds[u][r] = own < n ? e * ds[u][r] : 0.f;
             }
         }
         const vec8 p_op = operand(In{}, pr[0], pr[1]), ds_op = operand(In{}, ds[0], ds[1]);
@@ -526,8 +652,8 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
     }
     if (own < n) {
         const int64_t at = ((int64_t)s + own) * p.grad_tok + head + 16 * g;
-        store_row(In{}, p.dk + at, acc_k, p.scale);
-        store_row(In{}, p.dv + at, acc_v, 1.0f);
+        store_row(In{}, p.dk + at, acc_k, p.scale * power2(-fit));
+        store_row(In{}, p.dv + at, acc_v, kFit<In> ? power2(-kFitP) : 1.0f);
     }
     __syncthreads();
     // dQ^T += K^T dS^T: in the transposed read this wavefront's columns are the queries 16 (col / 4) + 4 wave + col % 4
@@ -541,7 +667,7 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) acc_q[dt] = In::mfma(transposed(k0, dt, bb), ds_op, acc_q[dt]);
     }
-    if (query < n) store_row(In{}, p.dq + ((int64_t)s + query) * p.grad_tok + head + 16 * g, acc_q, p.scale);
+    if (query < n) store_row(In{}, p.dq + ((int64_t)s + query) * p.grad_tok + head + 16 * g, acc_q, p.scale * power2(-fit));
 }
 
 template <typename In, int CB>
