@@ -342,7 +342,8 @@ int ragged_rope_frequencies(double* freqs, int pairs, double base, int scaling, 
 
 /*
  * ragged_attn_lse -- ragged_attn_strided that also writes what the backward pass needs of it:
- *   lse        [T, H]   fp32 out: lse[s + r, h] = ln sum_j exp( scale * q[s+r, h, :] . k[s+j, h, :] ); rows >= T are left untouched
+ *   lse        [T, H]   fp32 out: lse[s + r, h] = ln sum_j exp( scale * q[s+r, h, :] . k[s+j, h, :] ); rows >= T are left untouched, and so
+ *                        may be, as in o, rows at positions >= max_seqlen of a sequence that is longer than this bound
  * o has the dtype of the inputs and is bit-identical to ragged_attn_strided's with the same arguments.
  */
 int ragged_attn_lse(const void* q, const void* k, const void* v, void* o, float* lse, const int32_t* cu_seqlens, int B, int max_seqlen, int H,
@@ -358,8 +359,11 @@ int ragged_attn_lse(const void* q, const void* k, const void* v, void* o, float*
  *   dq, dk, dv [T, H, D]  out (dt), grad_tok_stride elements between tokens (for example the slices of a fused [T, 3, H, D] buffer);
  *                         they must not overlap any input or each other (the same address is refused, RAGGED_ERR_UNSUPPORTED).  Rows >= T
  *                         are left untouched
- *   max_seqlen            an upper bound on every n_i; gradients of rows at positions >= max_seqlen of a longer sequence may be left
- *                         uncomputed (such a row then stays untouched as a whole)
+ *   max_seqlen            an upper bound on every n_i.  Of a sequence that is longer all the same, gradients of rows at positions >= max_seqlen may be
+ *                         left uncomputed (such a row then stays untouched as a whole); dq of the rows below is right, and dk and dv, sums over all
+ *                         of its queries, are right only where o and lse hold all of its rows.  A forward call with the same bound has left the
+ *                         last ones unwritten, and these dk and dv then mean nothing (ragged_attn_checked tells whether a bound holds).  Other
+ *                         sequences are right either way
  *
  * Supported: D = 64, dt = F16 or BF16; every token row on a 16-byte boundary; strides as for ragged_attn_strided (grad_tok_stride as
  * out_tok_stride).  max_seqlen <= 64 * 32767 and half of the work-groups of ragged_attn's limit.  Products on MFMA with fp32 sums;
@@ -367,7 +371,7 @@ int ragged_attn_lse(const void* q, const void* k, const void* v, void* o, float*
  * overflows and small ones keep their bits (F dS loses them below 2^-14, some 2^-23 of the largest): a gradient is infinite only where its own value is.
  * In sequences of up to 32 rows rowsum(dO * o) is formed as rowsum(P * dO v^T) in fp32 (the rounding of o does not tell), and a sequence of
  * one row gets dq = dk = 0.
- * No atomics: results are bit-reproducible, and those of a sequence do not depend on the other sequences or on max_seqlen.
+ * No atomics: results are bit-reproducible, and those of a sequence do not depend on the other sequences or, as long as it holds, on max_seqlen.
  */
 int ragged_attn_backward(const void* q, const void* k, const void* v, const void* o, const void* d_o, const float* lse, void* dq, void* dk,
                          void* dv, const int32_t* cu_seqlens, int B, int max_seqlen, int H, int D, int64_t in_tok_stride,

@@ -536,7 +536,8 @@ def _attn_backward_args(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen
 
 def ragged_attn_backward(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen: int, scale: float, stream=None) -> None:
     """Gradients dq, dk, dv of ragged_attn_lse's q, k, v from its output o, that output's gradient d_o and lse.  q, k, v share
-    a token stride, o and d_o share one, dq, dk, dv share one."""
+    a token stride, o and d_o share one, dq, dk, dv share one.  max_seqlen has to hold for every sequence in both calls: dk and dv of
+    a longer one are sums over rows of o and lse that the forward call has not written."""
     _check("ragged_attn_backward", _native().ragged_attn_backward(
         *_attn_backward_args(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen, scale, stream)))
 
