@@ -563,8 +563,9 @@ class AttentionTraining:
         h = LN(x); q, k, v = h Wqkv^T + b; q, k = rope(q, k); a = attention; x = x + a Wo^T + b
     forward, back from a given gradient of the last x, and the gradients of all parameters clipped by their norm into one
     fp32 buffer.  A patch's position is its place in the square grid of the unpruned image, found through gather_idx; the class token is
-    at the origin.  Every launch of this library takes the row count from the device; rows beyond it stay zero in every buffer, so the
-    weights' gradients are plain library products over the whole buffers.  The input gradient of a linear layer is ragged_linear with
+    at the origin.  Every launch of this library takes the row count from the device.  The
+    weights' gradients are plain library products over the whole buffers, for which every step clears what they read: rows beyond the
+    count may hold those of an earlier step with more tokens.  The input gradient of a linear layer is ragged_linear with
     the transposed weight."""
 
     def __init__(self, w, depth: int = 4, max_norm: float = 1.0):
@@ -608,11 +609,13 @@ class AttentionTraining:
         outs = [o.view_as(g) for o, g in zip(self.clipped.split([g.numel() for g in flat]), flat)]
         self.plan, self.norm = binding.GradPlan(flat, outs), z(1, dt=torch.float64)
         self.ones = torch.ones(1, cap, dtype=tdt, device=dev)
+        self.row_numbers, self.beyond = torch.arange(cap, dtype=torch.int32, device=dev)[:, None], z(cap, 1, dt=torch.bool)
         torch.cuda.synchronize()
 
     def forward(self):
         b, w, rows = self.b, self.w, self.rows
         C = w.C
+        self.torch._foreach_zero_([*self.h, *self.a, self.d_qkv])
         b.ragged_pack(self.x_in, self.keep, self.x[0], self.cu, self.gidx)
         for i, p in enumerate(self.params):
             q, k, v = self.qkv[i].unbind(1)
@@ -623,10 +626,12 @@ class AttentionTraining:
             b.ragged_linear(self.a[i].view(self.cap, C), p["w_o"], p["b_o"], self.x[i], self.x[i + 1], rows)
 
     def backward(self, d_last):
-        """d_last [cap, C]: the gradient of the last x, zero beyond the valid rows."""
+        """d_last [cap, C]: the gradient of the last x; rows beyond the valid ones do not count, whatever they hold."""
         b, w, rows, torch = self.b, self.w, self.rows, self.torch
         C = w.C
         self.d_x.copy_(d_last)
+        torch.ge(self.row_numbers, rows, out=self.beyond)
+        self.d_x.masked_fill_(self.beyond, 0)
         for i in reversed(range(self.depth)):
             p, g = self.params[i], self.grads[i]
             q, k, v = self.qkv[i].unbind(1)
