@@ -586,7 +586,7 @@ class AttentionTraining:
         self.params = []
         for i in range(depth):
             p = {k: v.to(dev) for k, v in wl.block_weights(C, 64, w.dtype, 2000 + i).items() if k in ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o")}
-            p["w_qkv_t"], p["w_o_t"] = p["w_qkv"].t().contiguous(), p["w_o"].t().contiguous()
+            p["w_qkv_t"], p["w_o_t"] = z(C, 3 * C), z(C, C)     # (written by every backward pass)
             self.params.append(p)
         side = max(1, math.isqrt(N - 1)) if N > 1 else 1
         patch = torch.arange(N) - 1
@@ -634,6 +634,8 @@ class AttentionTraining:
         self.d_x.masked_fill_(self.beyond, 0)
         for i in reversed(range(self.depth)):
             p, g = self.params[i], self.grads[i]
+            p["w_qkv_t"].copy_(p["w_qkv"].t())                 # of the weights as they are now: an optimiser changes them every step
+            p["w_o_t"].copy_(p["w_o"].t())
             q, k, v = self.qkv[i].unbind(1)
             dq, dk, dv = self.d_qkv.unbind(1)
             d_a, d_qkv = self.d_a.view(self.cap, C), self.d_qkv.view(self.cap, 3 * C)
