@@ -125,15 +125,29 @@ void grad_squares_kernel(const GradChunk* __restrict__ table, int chunks, double
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
+// The factor as fp32, with a power of two of its own where it lies below fp32's normal numbers: gradients of 1e38 clipped to a norm of 1 have 1e-40,
+// in fp32 off by 2^-17 of itself, and outputs that are ordinary numbers.  (One instruction more a value; both kernels are bound by memory.)
+struct Factor {
+    float times;                                               // then in [1/2, 1)
+    int power;
+    static __device__ __forceinline__ Factor from(double f) {
+        if (fabs(f) >= 0x1p-126) return {(float)f, 0};
+        int power;
+        const float times = (float)frexp(f, &power);
+        return {times, power};
+    }
+    __device__ __forceinline__ float of(float v) const { return __builtin_ldexpf(v * times, power); }
+};
+
 template <int SRC, int DST, bool BYPASS>
-__device__ __forceinline__ void chunk_scale(const void* src, void* dst, int n, float factor) {
+__device__ __forceinline__ void chunk_scale(const void* src, void* dst, int n, Factor by) {
     constexpr int W = DST == RAGGED_F32 ? 4 : 8;               // 16 bytes of output
     typedef GradLine<SRC, W> In;
     typedef GradLine<DST, W> Out;
     auto scale = [&](const typename In::line& w, int i) {
         typename Out::line v;
 #pragma unroll
-        for (int e = 0; e < W; ++e) v[e] = Grad<DST>::rounded(Grad<SRC>::value(w[e]) * factor);
+        for (int e = 0; e < W; ++e) v[e] = Grad<DST>::rounded(by.of(Grad<SRC>::value(w[e])));
         Out::template store<BYPASS>(dst, i, v);
     };
     const int whole = n / W * W;
@@ -148,12 +162,12 @@ __device__ __forceinline__ void chunk_scale(const void* src, void* dst, int n, f
     }
     for (; i < whole; i += kStep) scale(In::load(src, i), i);
     if (whole + (int)threadIdx.x < n)
-        Out::store1(dst, whole + threadIdx.x, Grad<DST>::rounded(Grad<SRC>::value(In::load1(src, whole + threadIdx.x)) * factor));
+        Out::store1(dst, whole + threadIdx.x, Grad<DST>::rounded(by.of(Grad<SRC>::value(In::load1(src, whole + threadIdx.x)))));
 }
 template <int SRC, bool BYPASS>
-__device__ __forceinline__ void chunk_scale(const GradChunk& t, float factor) {
-    if (t.dst_dt == RAGGED_F32) chunk_scale<SRC, RAGGED_F32, BYPASS>(t.src, t.dst, t.n, factor);
-    else chunk_scale<SRC, SRC, BYPASS>(t.src, t.dst, t.n, factor);
+__device__ __forceinline__ void chunk_scale(const GradChunk& t, Factor by) {
+    if (t.dst_dt == RAGGED_F32) chunk_scale<SRC, RAGGED_F32, BYPASS>(t.src, t.dst, t.n, by);
+    else chunk_scale<SRC, SRC, BYPASS>(t.src, t.dst, t.n, by);
 }
 
 template <bool BYPASS>
@@ -174,14 +188,14 @@ void grad_scale_kernel(const GradChunk* __restrict__ table, int chunks, const do
     // a norm that is no number or infinite clips nothing: the caller sees it in the norm
     double clip = isfinite(norm) ? (double)max_norm / (norm + 1e-6) : 1.0;
     clip = clip < 1.0 ? clip : 1.0;
-    const float factor = (float)(clip * (double)scale);
+    const Factor by = Factor::from(clip * (double)scale);
     for (; c >= 0; c -= gridDim.x) {
         const GradChunk t = next;
         if (c >= (int)gridDim.x) next = table[c - gridDim.x];
-        if (!t.dst || (t.dst == t.src && factor == 1.0f)) continue;
-        if (t.src_dt == RAGGED_F32) chunk_scale<RAGGED_F32, BYPASS>(t, factor);
-        else if (t.src_dt == RAGGED_F16) chunk_scale<RAGGED_F16, BYPASS>(t, factor);
-        else chunk_scale<RAGGED_BF16, BYPASS>(t, factor);
+        if (!t.dst || (t.dst == t.src && by.times == 1.0f)) continue;
+        if (t.src_dt == RAGGED_F32) chunk_scale<RAGGED_F32, BYPASS>(t, by);
+        else if (t.src_dt == RAGGED_F16) chunk_scale<RAGGED_F16, BYPASS>(t, by);
+        else chunk_scale<RAGGED_BF16, BYPASS>(t, by);
     }
 }
 
