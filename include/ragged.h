@@ -382,7 +382,7 @@ int ragged_attn_backward(const void* q, const void* k, const void* v, const void
  *     dx = (w - mean(w) - xh mean(w xh)) / sqrt(var + eps)  [+ residual_grad],   dgamma = sum_rows dy xh,   dbeta = sum_rows dy
  *
  *   x, dy, dx      [rows_cap, C] (dt); gamma [C] (dt); dx may be dy or residual_grad (each element is read before it is written, by
- *                  the same thread), and must not be x
+ *                  the same thread), and must not be x; other overlaps of what is written (workspace among it) are not allowed
  *   residual_grad  [rows_cap, C] (dt) or NULL: the gradient that reaches x past the LayerNorm (x + f(LN(x)))
  *   dgamma, dbeta  [C] fp32 out (0 where there are no rows)
  *   workspace      ragged_layernorm_backward_workspace(rows_cap, C) bytes, 16-byte aligned; its contents before and after the call mean

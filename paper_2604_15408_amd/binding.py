@@ -114,8 +114,44 @@ class _Ctypes:
     def here(device, *tensors):
         return all(t is None or t.device.index == device for t in tensors)
 
+    @staticmethod
+    def placed(device, written, *arguments):
+        memory = []
+        for one in arguments:
+            t, most = one if isinstance(one, tuple) else (one, None)
+            if t is not None and t.device.index != device:
+                return 1
+            memory.append(None if t is None or t.numel() == 0 else _memory(t, most))
+        return 2 if any(_overlap(a, b) for i, a in enumerate(memory[:written]) for b in memory[i + 1:]) else 0
+
     def __getattr__(self, name):
         return getattr(load(), name)
+
+
+def _memory(t: torch.Tensor, most=None):
+    """Memory of a tensor as (address, rows, bytes from row to row, bytes of a row); most: only its first bytes."""
+    size = t.element_size()
+    if t.is_contiguous():
+        n, step, length = 1, 0, t.numel() * size
+    else:
+        n, step, length = t.shape[0], t.stride(0) * size, (1 + sum((m - 1) * s for m, s in zip(t.shape[1:], t.stride()[1:]))) * size
+        if n > 1 and step < length:                            # (rows that run into each other: as one)
+            n, step, length = 1, 0, (n - 1) * step + length
+    return t.data_ptr(), n, step, length if most is None else min(length, most)
+
+
+def _overlap(a, b) -> bool:
+    """Whether any byte is in both.  Rows at different distances whose ranges meet count as overlapping."""
+    if a is None or b is None:
+        return False
+    if b[0] < a[0]:
+        a, b = b, a
+    if b[0] >= a[0] + (a[1] - 1) * a[2] + a[3]:
+        return False
+    if a[1] == 1 or (b[1] > 1 and a[2] != b[2]):
+        return True
+    behind = (b[0] - a[0]) % a[2]                              # of the first of b, behind the start of a row of a
+    return behind < a[3] or behind + b[3] > a[2]
 
 
 _marshal = None
@@ -425,6 +461,15 @@ def _here(*tensors) -> None:
         raise ValueError(f"a tensor is not on the current device (cuda:{device})")
 
 
+def _placed(written: int, *arguments) -> None:
+    """_here, and none of the first `written` arguments may share memory with another one: what a work-group writes others still read."""
+    device = _raw_device() if _raw_device is not None else torch.cuda.current_device()
+    wrong = (_marshal or _native()).placed(device, written, *arguments)
+    if wrong:
+        raise ValueError(f"a tensor is not on the current device (cuda:{device})" if wrong == 1 else
+                         "an output overlaps another output or an input")
+
+
 _ROPE_LAYOUT = {"half": 0, "interleaved": 1}
 _ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
 
@@ -466,7 +511,7 @@ def _rope_args(q, k, q_out, k_out, coords, freqs, index, layout, amplitude, inve
             None if index is None else dev(index, torch.int32, (n,)) or _dev(index, "index", torch.int32, (n,)),
             dev(freqs, torch.float64, None) or _dev(freqs, "freqs", torch.float64), freqs.numel(), _ROPE_LAYOUT[layout], float(amplitude),
             1 if inverse else 0, _DTYPE_CODE[dt], _stream(stream))
-    _here(q, k, q_out, k_out, coords, freqs, index, rows_dev)
+    _placed(2, q_out, k_out, None if (qop, qos) == (qp, qs) else q, None if (kop, kos) == (kp, ks) else k, coords, freqs, index, rows_dev)
     return args
 
 
@@ -495,7 +540,7 @@ def _attn_lse_args(q, k, v, o, lse, cu_seqlens, max_seqlen, scale, stream):
     op, out_tok = rows(o, dt, shape) or _token_rows(o, "o", dt, shape)
     if not in_tok == ks == vs:
         raise ValueError("q, k, v must share their token stride")
-    _here(q, k, v, o, lse, cu_seqlens)
+    _placed(2, o, lse, q, k, v, cu_seqlens)
     n, H, D = shape
     dev = (_marshal or _native()).dev
     return (qp, kp, vp, op, dev(lse, torch.float32, (n, H)) or _dev(lse, "lse", torch.float32, (n, H)),
@@ -526,7 +571,7 @@ def _attn_backward_args(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens, max_seqlen
     dvp, dvs = rows(dv, dt, shape) or _token_rows(dv, "dv", dt, shape)
     if not (in_tok == ks == vs and out_tok == dos and grad_tok == dks == dvs):
         raise ValueError("q, k, v must share their token stride, o and d_o theirs, dq, dk, dv theirs")
-    _here(q, k, v, o, d_o, lse, dq, dk, dv, cu_seqlens)
+    _placed(3, dq, dk, dv, q, k, v, o, d_o, lse, cu_seqlens)
     n, H, D = shape
     dev = (_marshal or _native()).dev
     return (qp, kp, vp, op, dop, dev(lse, torch.float32, (n, H)) or _dev(lse, "lse", torch.float32, (n, H)), dqp, dkp, dvp,
@@ -571,7 +616,8 @@ def _layernorm_backward_args(x, gamma, dy, dx, dgamma, dbeta, workspace, residua
             dev(dbeta, torch.float32, (C,)) or _dev(dbeta, "dbeta", torch.float32, (C,)),
             dev(workspace, None, None) or _dev(workspace, "workspace"), rows, None if rows_dev is None else _rows_dev(rows_dev), C, float(eps),
             _DTYPE_CODE[dt], _stream(stream))
-    _here(x, gamma, dy, dx, dgamma, dbeta, workspace, residual_grad, rows_dev)
+    _placed(4, dx, dgamma, dbeta, (workspace, need), x, gamma, None if args[4] == args[2] else dy, None if args[4] == args[3] else residual_grad,
+            rows_dev)
     return args
 
 

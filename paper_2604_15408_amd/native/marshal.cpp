@@ -94,6 +94,70 @@ PyObject* here(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Py_RETURN_TRUE;
 }
 
+// Memory of an argument: n rows of len bytes, step bytes apart.
+struct Memory {
+    const char* at;
+    int64_t n, step, len;
+    const char* end() const { return at + (n - 1) * step + len; }
+};
+Memory memory_of(const at::Tensor& t, int64_t most) {
+    const int64_t size = static_cast<int64_t>(t.element_size());
+    Memory m{static_cast<const char*>(t.data_ptr()), t.numel() == 0 ? 0 : 1, 0, t.numel() * size};
+    if (m.n && !t.is_contiguous()) {
+        m.len = size;
+        for (int64_t d = 1; d < t.dim(); ++d) m.len += (t.size(d) - 1) * t.stride(d) * size;
+        m.n = t.size(0);
+        m.step = t.stride(0) * size;
+        if (m.n > 1 && m.step < m.len) m = Memory{m.at, 1, 0, (m.n - 1) * m.step + m.len};       // (rows that run into each other: as one)
+    }
+    if (m.len > most) m.len = most;
+    return m;
+}
+// Whether any byte is in both.  Rows at different distances whose ranges meet count as overlapping.
+bool overlap(Memory a, Memory b) {
+    if (a.n == 0 || b.n == 0) return false;
+    if (b.at < a.at) std::swap(a, b);
+    if (b.at >= a.end()) return false;
+    if (a.n == 1 || (b.n > 1 && a.step != b.step)) return true;
+    const int64_t behind = (b.at - a.at) % a.step;             // of the first of b, behind the start of a row of a
+    return behind < a.len || behind + b.len > a.step;
+}
+
+// placed(device, written, argument, ...) -> 0; 1: an argument is not on that device; 2: one of the first `written` shares memory with another.
+// Arguments are tensors, None, or (tensor, bytes) where only its first bytes are used.
+PyObject* placed(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    constexpr Py_ssize_t kMost = 16;
+    const long device = n > 1 ? PyLong_AsLong(args[0]) : -1, written = n > 1 ? PyLong_AsLong(args[1]) : -1;
+    if (PyErr_Occurred()) return nullptr;
+    if (n < 2 || n - 2 > kMost) {
+        PyErr_SetString(PyExc_TypeError, "placed takes a device, a count and up to 16 arguments");
+        return nullptr;
+    }
+    try {
+        Memory memory[kMost];
+        for (Py_ssize_t i = 0; i < n - 2; ++i) {
+            PyObject* one = args[i + 2];
+            memory[i] = Memory{nullptr, 0, 0, 0};
+            if (one == Py_None) continue;
+            int64_t most = INT64_MAX;
+            if (PyTuple_Check(one) && PyTuple_GET_SIZE(one) == 2) {
+                most = PyLong_AsLongLong(PyTuple_GET_ITEM(one, 1));
+                if (PyErr_Occurred()) return nullptr;
+                one = PyTuple_GET_ITEM(one, 0);
+            }
+            if (!THPVariable_Check(one) || THPVariable_Unpack(one).device().index() != device) return PyLong_FromLong(1);
+            memory[i] = memory_of(THPVariable_Unpack(one), most);
+        }
+        for (Py_ssize_t i = 0; i < written && i < n - 2; ++i)
+            for (Py_ssize_t j = i + 1; j < n - 2; ++j)
+                if (overlap(memory[i], memory[j])) return PyLong_FromLong(2);
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+    return PyLong_FromLong(0);
+}
+
 template <typename T>
 bool convert(PyObject* o, T& out) {
     if constexpr (std::is_pointer_v<T>) {
@@ -133,6 +197,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) { return invoke(
 PyMethodDef methods[] = {
     {"dev", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&dev)), METH_FASTCALL, nullptr},
     {"rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&rows)), METH_FASTCALL, nullptr},
+    {"placed", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&placed)), METH_FASTCALL, nullptr},
     {"here", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&here)), METH_FASTCALL, nullptr},
     ENTRY(ragged_pack), ENTRY(ragged_attn), ENTRY(ragged_attn_strided), ENTRY(ragged_attn_checked), ENTRY(ragged_attn_padded),
     ENTRY(ragged_unpack), ENTRY(ragged_repack), ENTRY(ragged_cls_extract), ENTRY(ragged_pack_attn_unpack), ENTRY(ragged_linear),
