@@ -474,6 +474,13 @@ _ROPE_LAYOUT = {"half": 0, "interleaved": 1}
 _ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
 
 
+def _choice(choices: dict, given, name: str) -> int:
+    code = choices.get(given) if isinstance(given, str) else None
+    if code is None:
+        raise ValueError(f"{name} is {given!r}, expected one of {', '.join(choices)}")
+    return code
+
+
 def rope_frequencies(pairs: int, base: float = 10000.0, axes: int = 1, scaling: str = "none", factor: float = 1.0,
                      original_length: float = 0.0, fast: float = 32.0, slow: float = 1.0) -> torch.Tensor:
     """freqs of ragged_rope as a float64 CPU tensor [pairs]: each of the axes has pairs / axes of them, from 1 down to
@@ -482,7 +489,7 @@ def rope_frequencies(pairs: int, base: float = 10000.0, axes: int = 1, scaling: 
         raise ValueError(f"{pairs} pairs cannot be shared out over {axes} axes")
     one = torch.empty(pairs // axes, dtype=torch.float64)
     _check("ragged_rope_frequencies", _native().ragged_rope_frequencies(
-        one.data_ptr(), pairs // axes, float(base), _ROPE_SCALING[scaling], float(factor), float(original_length), float(fast), float(slow)))
+        one.data_ptr(), pairs // axes, float(base), _choice(_ROPE_SCALING, scaling, "scaling"), float(factor), float(original_length), float(fast), float(slow)))
     return one.repeat(axes)
 
 
@@ -509,7 +516,7 @@ def _rope_args(q, k, q_out, k_out, coords, freqs, index, layout, amplitude, inve
     args = (qp, kp, qop, kop, n, None if rows_dev is None else _rows_dev(rows_dev), hq, hk, d, qs, ks, qos, kos,
             dev(coords, torch.float32, None) or _dev(coords, "coords", torch.float32), lines, axes,
             None if index is None else dev(index, torch.int32, (n,)) or _dev(index, "index", torch.int32, (n,)),
-            dev(freqs, torch.float64, None) or _dev(freqs, "freqs", torch.float64), freqs.numel(), _ROPE_LAYOUT[layout], float(amplitude),
+            dev(freqs, torch.float64, None) or _dev(freqs, "freqs", torch.float64), freqs.numel(), _choice(_ROPE_LAYOUT, layout, "layout"), float(amplitude),
             1 if inverse else 0, _DTYPE_CODE[dt], _stream(stream))
     _placed(2, q_out, k_out, None if (qop, qos) == (qp, qs) else q, None if (kop, kos) == (kp, ks) else k, coords, freqs, index, rows_dev)
     return args
