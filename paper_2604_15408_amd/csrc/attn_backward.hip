@@ -405,18 +405,6 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
     }
 }
 
-// Sum over the 16 lanes that share a row of scores (lanes 16 g .. 16 g + 15), in every one of them.
-template <int kCtrl>
-__device__ __forceinline__ float rotated(float v) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, true));
-}
-__device__ __forceinline__ float row_sum(float v) {
-    v += rotated<0x128>(v);                                    // row_ror:8
-    v += rotated<0x124>(v);
-    v += rotated<0x122>(v);
-    return v + rotated<0x121>(v);
-}
-
 // A whole sequence of at most kFewKeys rows: as whole_sequence, but delta is the sum over the keys of P dP in fp32, over the lanes of a
 // wavefront and then over the two that have keys; o is not read.  The same sum from the rounded o is off by u |dO| |o|, and the fewer the
 // keys the more that is beside the rounding of dS: with two keys dQ and dK were off by 3.3 thousandths in bf16, now by 2.4, as everywhere
@@ -487,7 +475,7 @@ __device__ __forceinline__ void few_keys(const BackwardArgs& p, uint4* lds, int 
                 const bool there = own < n && 16 * kt + 4 * g + r < n;
                 pr[kt][r] = there ? e : 0.f;
                 ds[kt][r] = there ? ds[kt][r] : 0.f;
-                part[kt][r] = row_sum(pr[kt][r] * ds[kt][r]);
+                part[kt][r] = lanes_sum_f32<16>(pr[kt][r] * ds[kt][r]);
             }
             if (col == 0) parts[wave * (kFewKeys / 4) + 4 * kt + g] = part[kt];
         }
@@ -495,10 +483,10 @@ __device__ __forceinline__ void few_keys(const BackwardArgs& p, uint4* lds, int 
             float most = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(ds[e / 4][e % 4]));
-            most = fmaxf(most, rotated<0x128>(most));
-            most = fmaxf(most, rotated<0x124>(most));
-            most = fmaxf(most, rotated<0x122>(most));
-            most = quad_max(fmaxf(most, rotated<0x121>(most)));
+            most = fmaxf(most, dpp_f32<0x128>(most));
+            most = fmaxf(most, dpp_f32<0x124>(most));
+            most = fmaxf(most, dpp_f32<0x122>(most));
+            most = quad_max(fmaxf(most, dpp_f32<0x121>(most)));
             if (lane == 0) votes[wave] = as_u32(most);
         }
     }
