@@ -6,7 +6,8 @@
 // cosines and sines in LDS while those are on their way, and rotates.
 //
 // Angles.  coordinate * frequency can be 10^6 radians, where the distance of fp32 numbers is 0.06.  The product is formed in fp64 as a
-// number of turns (error 2^-53 of it), brought to [-1/2, 1/2] by subtracting the nearest whole number, and only then rounded to fp32.
+// number of turns (three roundings, of 1 / (2 pi) and of two products: off by 3 * 2^-53 of it at most), brought to [-1/2, 1/2] by subtracting
+// the nearest whole number, and only then rounded to fp32.
 #include "common.h"
 #include "linear_kernel.h"
 
