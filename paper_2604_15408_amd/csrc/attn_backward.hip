@@ -22,7 +22,8 @@
 // a work-group of keys a quarter of its time (same case 112 us for the keys alone, 82 without).  - delta is where the sum dP starts.
 //
 // P and dS are rounded to the input type for the second products, as the gradients themselves are in the end: a sum of n terms
-// whose signs are mixed is off by about as much as its own rounding.  Sums are fp32.
+// whose signs are mixed is off by about as much as its own rounding (2.4 thousandths in bf16, 0.30 in fp16; a rounding of the exact gradients 1.7
+// and 0.21, which both kept as hi + lo would reach in 1.7 to 1.8 times the time).  Sums are fp32.
 //
 // fp16 has the bits for that and not the range: P = 1/n is below its normal numbers beyond 16 384 keys, dS overflows at 65 504 where dQ and dK
 // need not, and vanishes where gradients are small.  So P is rounded as 2^15 P, and dS as F dS; both are taken out of the fp32 sums.
@@ -34,8 +35,9 @@
 // multiplication more past keys (from F P to 2^15 P), and none past queries.  Launches of fp16 take 2 to 8 % more for it, most of it for the
 // sample (64 x 128 28.5 -> 30.4 us, 128 x about 100 38.2 -> 41.1, 64 x 197 55.6 -> 58, 32 x 577 144 -> 149, 256 x 30 19.4 -> 20.4).
 //
-// us now (gradients alone, H = 12): 32 x 577 bf16 141 (82 GFLOP in five products, 115 in the seven of this form: 0.8 PFLOP/s, where a loop of
-// products alone sustains 1.3), 64 x 197 fp16 52 (155 MB of rows: 26 us at the rate of a copy), 32 x about 40 bf16 6.7.
+// us now (gradients alone, H = 12, by the card): 32 x 577 bf16 138 to 150 (82 GFLOP in five products, 115 in the seven of this form: 0.77 to
+// 0.83 PFLOP/s, where a loop of products alone sustains 1.3), 64 x 197 bf16 52, fp16 58 (155 MB of rows: 26 us at the rate of a copy), 32 x about
+// 40 bf16 6.4.
 #include <type_traits>
 
 #include "attn_parts.h"
@@ -46,9 +48,10 @@
 namespace ragged {
 namespace {
 
-// Launches of at most this many work-groups of 128 rows take work-groups of 64 (CB = 1): CUs would be idle.  us with 64 / 128 rows: 2 x 197
-// tokens, 3 heads 5.7 / 7.6, 4 x 197, 12 heads (192 groups) 8.8 / 10.7, 8 x 197 (384) 12.5 / 13.2, 16 x 128 (384) 10.2 / 10.5; beyond, 32 x 197 at
-// keep 0.5 (1536) 15.2 / 14.4, 64 x 197 63 / 55, 32 x 577 184 / 144.
+// Launches of at most this many work-groups of 128 rows take work-groups of 64 (CB = 1): CUs would be idle.  us with 64 / 128 rows, bf16: 2 x 197
+// tokens, 3 heads 7.7 / 9.8, 4 x 197, 12 heads (192 groups) 9.5 / 10.7, 8 x 197 (384) 12.7 / 12.8, 16 x 128 (384) 10.1 / 10.4; beyond, 32 x 197 at
+// keep 0.5 (1536) 15.3 / 13.1, 64 x 197 64 / 53, 32 x 577 186 / 143 (fp16 the same way: 8.4 / 10.4, 10.6 / 11.4, 13.8 / 14.0, 10.8 / 11.4; 16.4 / 13.9,
+// 71 / 57, 197 / 155).
 constexpr int kSmallGroups = 512;
 // (image, head) pairs of a dispatch batch: all the work-groups of a batch come before the next one's, those of a pair on one XCD.  As many
 // pairs as have their rows in three quarters of that XCD's 4 MB L2, so that the work-groups of a pair read them there; those of 512, as in
@@ -408,7 +411,7 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
 // A whole sequence of at most kFewKeys rows: as whole_sequence, but delta is the sum over the keys of P dP in fp32, over the lanes of a
 // wavefront and then over the two that have keys; o is not read.  The same sum from the rounded o is off by u |dO| |o|, and the fewer the
 // keys the more that is beside the rounding of dS: with two keys dQ and dK were off by 3.3 thousandths in bf16, now by 2.4, as everywhere
-// above 40.  It costs a second round through LDS, us with o / with P dP: 32 x 12 tokens 4.4 / 4.6, 32 x 30 4.9 / 5.3, 256 x 30
+// above 40.  It costs a second round through LDS, us in bf16 with o / with P dP: 32 x 12 tokens 4.4 / 4.6, 32 x 30 4.9 / 5.3, 256 x 30
 // 19.9 / 19.5; of all sequences up to 64 rows (four wavefronts, 64 queries each) 1 us of 6 to 12, hence the threshold.
 constexpr int kFewKeys = 32;
 template <typename In>

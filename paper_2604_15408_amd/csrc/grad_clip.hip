@@ -8,8 +8,8 @@
 // Squares are formed and added in fp64: they are exact there (24-bit values), no gradient's square overflows or vanishes,
 // and with one conversion and one fma a value the kernel stays bound by memory.
 //
-// us (both kernels): 151 M bf16 values into fp32 194 (squares 46: 6.6 TB/s; scaling 148: 6.1 TB/s of reads and writes), fp32 into fp32 304;
-// 5.5 M fp32 values 16.4 (5.3 and 9.0 in the kernels); 180 thousand 9.
+// us (both kernels): 151 M bf16 values into fp32 189 (squares 50: 6.0 TB/s; scaling 138: 6.6 TB/s of reads and writes), fp32 into fp32 297;
+// 5.5 M fp32 values 14.2 to 14.9 (5.5 and 9.1 in the kernels by the profiler); 0.7 M bf16 into fp32 8.
 #include "common.h"
 #include "linear_kernel.h"
 
@@ -19,7 +19,8 @@ namespace {
 constexpr int kChunk = 16384;                                  // values of a chunk (151 M bf16 into fp32: 8192 as fast, 32768 213 us)
 // Outputs of more values than this go past the caches, which keeps the gradients there for the second reading: 151 M values 242 -> 206 us;
 // that one then leaves them to others as well: 194.
-// Fewer are left there for the optimiser (38 M into fp32 55 us, 53 past them).
+// Fewer are left there for the optimiser (38 M into fp32 55 us, 53 past them).  Every chunk counts as a whole one: of thousands of small
+// tensors, which are more than 2048 chunks with fewer values, the outputs go past the caches as well.
 constexpr int64_t kClipBypass = 32 << 20;
 constexpr int kClipGroups = 1024;                              // work-groups (and partial sums) at most
 static_assert(kClipGroups * 8 <= RAGGED_GRAD_WORKSPACE, "one fp64 sum for each work-group");
