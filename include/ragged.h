@@ -367,8 +367,8 @@ int ragged_attn_lse(const void* q, const void* k, const void* v, void* o, float*
  *
  * Supported: D = 64, dt = F16 or BF16; every token row on a 16-byte boundary; strides as for ragged_attn_strided (grad_tok_stride as
  * out_tok_stride).  max_seqlen <= 64 * 32767 and half of the work-groups of ragged_attn's limit.  Products on MFMA with fp32 sums;
- * P and dS are rounded to dt in between; with fp16 as 2^15 P and F dS, where F is a power of two that the kernel takes from dO and v, so that neither
- * overflows and small ones keep their bits (F dS loses them below 2^-14, some 2^-23 of the largest): a gradient is infinite only where its own value is.
+ * P and dS are rounded to dt in between; with fp16 as 2^15 P and F dS, where F is a power of two that the kernel takes from dO and v, 1 or more unless
+ * dS would overflow with it: neither leaves the type's range, F dS loses bits below 2^-14 only, and a gradient is infinite only where its own value is.
  * In sequences of up to 32 rows rowsum(dO * o) is formed as rowsum(P * dO v^T) in fp32 (the rounding of o does not tell), and a sequence of
  * one row gets dq = dk = 0.
  * No atomics: results are bit-reproducible, and those of a sequence do not depend on the other sequences or, as long as it holds, on max_seqlen.

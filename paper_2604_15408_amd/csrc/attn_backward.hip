@@ -28,9 +28,10 @@
 // fp16 has the bits for that and not the range: P = 1/n is below its normal numbers beyond 16 384 keys, dS overflows at 65 504 where dQ and dK
 // need not, and vanishes where gradients are small.  So P is rounded as 2^15 P, and dS as F dS; both are taken out of the fp32 sums.
 // |dS| <= |dP - delta| <= 2 |dO| |v|, and F is the power of two with which 2 |dO| |v| is below 2^14, |dO| and |v| being the lengths of several
-// rows as one vector.  Up to 64 rows that is all of them.  Of a longer sequence it is 4 rows, spread evenly over it, so that F is the same in every
-// work-group and launch (past queries a query's own dO): with N(0, 1) rows F = 16 and |F (dP - delta)| is up to 2^9.  Where far larger rows come
-// all the same, the sums of a column end as infinities or no numbers, all of them: such columns are gone through again with 2^-16 F, down to
+// rows as one vector.  From 33 to 64 rows that is all of them; up to 32 F comes from the largest |P dP| instead, which is there, as is, if F were
+// below 1, the largest |dS| of 33 to 64 rows.  Of a longer sequence it is 4 rows, spread evenly over it, so that F is the same in every
+// work-group and launch (past queries a query's own dO), and 1 at least: with N(0, 1) rows F = 16 and |F (dP - delta)| is up to 2^9.  Where far larger
+// dS come all the same, the sums of a column end as infinities or no numbers, all of them: such columns are gone through again with 2^-16 F, down to
 // 2^-24, with which no dS overflows; the others have been stored.  F is in the exponent that P is formed with, so that the loop has one
 // multiplication more past keys (from F P to 2^15 P), and none past queries.  Launches of fp16 take 2 to 8 % more for it, most of it for the
 // sample (64 x 128 28.5 -> 30.4 us, 128 x about 100 38.2 -> 41.1, 64 x 197 55.6 -> 58, 32 x 577 144 -> 149, 256 x 30 19.4 -> 20.4).
@@ -121,6 +122,12 @@ __device__ __forceinline__ int fit_within(int fit) { return fit < kFitLast ? kFi
 __device__ __forceinline__ int fit_of(float squares_do, float squares_v) {
     const float a = squares_do == 0.f ? 1.f : squares_do, b = squares_v == 0.f ? 1.f : squares_v;
     return fit_within(12 - (exponent(a * b) >> 1));            // 2 sqrt(a b) < 2^(exponent / 2 + 2)
+}
+__device__ __forceinline__ float wave_max(float v) {
+    v = fmaxf(v, dpp_f32<0x128>(v));
+    v = fmaxf(v, dpp_f32<0x124>(v));
+    v = fmaxf(v, dpp_f32<0x122>(v));
+    return quad_max(fmaxf(v, dpp_f32<0x121>(v)));
 }
 __device__ __forceinline__ float squares(const uint4& w) {
     const f16x8 v = as_vec8<f16x8>(w);
@@ -237,6 +244,7 @@ __device__ __forceinline__ void own_rows(const BackwardArgs& p, uint4* lds, int 
             // (4 times the square of a query's own row: what 4 such rows would have in the sample)
             fit[cb] = KEYS ? fit_of(size_do, size_v)
                            : fit_of(4.f * quad_sum(squares(own_b[cb][0]) + squares(own_b[cb][1])), size_v);
+            fit[cb] = fit[cb] < 0 ? 0 : fit[cb];               // (large rows need not count: one that nobody looks at does not)
             if (!KEYS) lse2[cb] -= (float)fit[cb];
         }
 #pragma unroll
@@ -464,6 +472,7 @@ __device__ __forceinline__ void few_keys(const BackwardArgs& p, uint4* lds, int 
     __syncthreads();
     f32x4 pr[2], ds[2], part[2];                               // 16 queries each
     if (active) {
+        float most = 0.f;                                      // fp16: the largest |P dP|
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             const uint32_t ra = q0 + row_rel + kt * 2048, rb = do0 + row_rel + kt * 2048;
@@ -478,18 +487,14 @@ __device__ __forceinline__ void few_keys(const BackwardArgs& p, uint4* lds, int 
                 const bool there = own < n && 16 * kt + 4 * g + r < n;
                 pr[kt][r] = there ? e : 0.f;
                 ds[kt][r] = there ? ds[kt][r] : 0.f;
-                part[kt][r] = lanes_sum_f32<16>(pr[kt][r] * ds[kt][r]);
+                const float share = pr[kt][r] * ds[kt][r];
+                part[kt][r] = lanes_sum_f32<16>(share);
+                most = fmaxf(most, fabsf(share));
             }
             if (col == 0) parts[wave * (kFewKeys / 4) + 4 * kt + g] = part[kt];
         }
-        if constexpr (kFit<In>) {                              // the largest |dP|; delta is no larger
-            float most = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(ds[e / 4][e % 4]));
-            most = fmaxf(most, dpp_f32<0x128>(most));
-            most = fmaxf(most, dpp_f32<0x124>(most));
-            most = fmaxf(most, dpp_f32<0x122>(most));
-            most = quad_max(fmaxf(most, dpp_f32<0x121>(most)));
+        if constexpr (kFit<In>) {
+            most = wave_max(most);
             if (lane == 0) votes[wave] = as_u32(most);
         }
     }
@@ -497,7 +502,8 @@ __device__ __forceinline__ void few_keys(const BackwardArgs& p, uint4* lds, int 
     int fit = 0;
     if constexpr (kFit<In>) {
         const float most = fmaxf(as_f32(votes[0]), as_f32(votes[1]));
-        fit = fit_within(most == 0.f ? 0 : 13 - exponent(most));                         // |dP - delta| < 2^(exponent + 2)
+        // |dS| <= |P dP| + P |delta| <= 33 times the largest |P dP|, which is below 2^(exponent + 1 - kFitP)
+        fit = fit_within(most == 0.f ? 0 : 8 + kFitP - exponent(most));
     }
     if (active) {
 #pragma unroll
@@ -600,17 +606,8 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
     int fit = 0;
     if constexpr (kFit<In>)
         fit = fit_of((sums[0] + sums[1]) + (sums[2] + sums[3]), (sums[4] + sums[5]) + (sums[6] + sums[7]));
-    f32x4 acc_k[4], acc_v[4];
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt) acc_k[dt] = acc_v[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto transposed = [&](uint32_t tile, int dt, int bb) {
-        const uint32_t a = tile + (((dt & 2) ? tr_rel ^ 16u : tr_rel) + 8 * (dt & 1) + bb * 32 * 128);
-        const uint2 lo = __builtin_bit_cast(uint2, lds_read_tr(a)), hi = __builtin_bit_cast(uint2, lds_read_tr(a + 16 * 128));
-        return as_vec8<vec8>(make_uint4(lo.x, lo.y, hi.x, hi.y));
-    };
-#pragma unroll
-    for (int bb = 0; bb < 2; ++bb) {
-        f32x4 pr[2], ds[2];
+    // 32 queries: P (fp16: 2^kFitP P) and, times `by`, dS
+    auto scores = [&](int bb, f32x4 (&pr)[2], f32x4 (&ds)[2], float by) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int kt = 2 * bb + u;
@@ -623,10 +620,39 @@ __device__ __forceinline__ void whole_sequence(const BackwardArgs& p, uint4* lds
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 pr[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(pr[u][r], c2, -row_lse[r]));
-                const float e = kFit<In> ? pr[u][r] * power2(fit - kFitP) : pr[u][r];
+                const float e = kFit<In> ? pr[u][r] * by : pr[u][r];
                 ds[u][r] = own < n ? e * ds[u][r] : 0.f;
             }
         }
+    };
+    if (kFit<In> && fit < 0) {                                 // rows that large need not count (nobody looks at some): by the largest |dS| itself
+        float most = 0.f;
+#pragma nounroll
+        for (int bb = 0; bb < 2; ++bb) {
+            f32x4 pr[2], ds[2];
+            scores(bb, pr, ds, power2(-kFitP));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(ds[e / 4][e % 4]));
+        }
+        most = wave_max(most);
+        __syncthreads();                                       // everyone has read the sums
+        if (lane == 0) sums[wave] = most;
+        __syncthreads();
+        most = fmaxf(fmaxf(sums[0], sums[1]), fmaxf(sums[2], sums[3]));
+        fit = fit_within(most == 0.f ? 0 : 14 - exponent(most));
+    }
+    f32x4 acc_k[4], acc_v[4];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) acc_k[dt] = acc_v[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto transposed = [&](uint32_t tile, int dt, int bb) {
+        const uint32_t a = tile + (((dt & 2) ? tr_rel ^ 16u : tr_rel) + 8 * (dt & 1) + bb * 32 * 128);
+        const uint2 lo = __builtin_bit_cast(uint2, lds_read_tr(a)), hi = __builtin_bit_cast(uint2, lds_read_tr(a + 16 * 128));
+        return as_vec8<vec8>(make_uint4(lo.x, lo.y, hi.x, hi.y));
+    };
+#pragma unroll
+    for (int bb = 0; bb < 2; ++bb) {
+        f32x4 pr[2], ds[2];
+        scores(bb, pr, ds, power2(fit - kFitP));
         const vec8 p_op = operand(In{}, pr[0], pr[1]), ds_op = operand(In{}, ds[0], ds[1]);
         // dS by keys: row own, queries 16 kt + 4 g .. + 3 in the same swizzled order as the other tiles
         const uint4 w = __builtin_bit_cast(uint4, ds_op);

@@ -142,3 +142,44 @@ def test_equal_scores_of_many_keys(zero):
     # sum over the keys of |dS x| is twice `size` at most (delta is the mean of what dP is); the rounding of o reaches delta
     bound = (U + e + long + 2.0 ** -17) * 2 * size + c / n * U * (dO * o).abs().sum(1).max() * (K if zero == "q" else Q).abs().sum(0)
     assert torch.all((got - want).abs() <= bound + U * want.abs() + OUT)
+
+
+@pytest.mark.parametrize("n", [20, 60, 200, 600, 3000])
+def test_a_huge_value_that_nobody_looks_at(n):
+    """The first key has v = 30 000 and probabilities of about e^-34: it decides nothing, and must not cost the others' dS their bits.  dS and result are
+    rounded once each, independently and to u: for terms of random signs an error of sqrt(2 / 3) u of the gradients' norm, with 2 u more than twice that."""
+    q, k, v, do = _inputs([n], 1, 34, 0.5, 0.5, 1.0)
+    q[:, :, 0], k[:, :, 0] = 8.0, 0.0
+    k[0, :, 0], v[0] = -34.0, 30000.0
+    _, dq, dk, dv = (t[:, 0].double() for t in _run(q, k, v, do, [n], 0.125))
+    Q, K, V, dO = (t[:, 0].double() for t in (q, k, v, do))
+    P = torch.softmax(0.125 * (Q @ K.t()), -1)
+    dP = dO @ V.t()
+    dS = P * (dP - (P * dP).sum(-1, keepdim=True))
+    for got, want in ((dq, 0.125 * (dS @ K)), (dk[1:], 0.125 * (dS.t() @ Q)[1:]), (dv[1:], (P.t() @ dO)[1:])):
+        assert (got - want).norm() <= 2 * U * want.norm() + OUT * want.numel() ** 0.5, float((got - want).norm() / want.norm())
+
+
+@pytest.mark.parametrize("what", ["do", "v", "both"])
+def test_second_attempts_have_the_same_bits_in_every_launch(what):
+    """Rows far larger than those that the size is taken from: in a launch of work-groups of 64 rows and among many of 128."""
+    n, many = 241, 70
+    q, k, v, do = _inputs([n], 3, 35, 2.0, 2.0 ** -2, 1.0)
+    rare = (torch.arange(n) % 80 == 0)[:, None, None]
+    if what != "v":
+        do = (do.float() * torch.where(rare, 2.0 ** -11, 2.0 ** 9)).half()
+    if what != "do":
+        v = (v.float() * torch.where(rare, 2.0 ** -14, 2.0 ** 3)).half()
+    o, *few = _run(q, k, v, do, [n], 0.125)
+    _check(q, k, v, do, [n], 0.125, [o, *few])
+    lot = [t.repeat(many, 1, 1).to(DEV) for t in (q, k, v, do, o)]
+    # the statistics of the first launch, whose own last place may differ from launch to launch
+    one_o, one_lse = torch.empty_like(q, device=DEV), torch.empty(n, 3, device=DEV)
+    cu = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    binding.ragged_attn_lse(*(t.to(DEV) for t in (q, k, v)), one_o, one_lse, cu, n, 0.125)
+    assert torch.equal(one_o.cpu(), o)
+    grads = [torch.zeros_like(lot[0]) for _ in range(3)]
+    ends = torch.arange(0, n * many + 1, n, dtype=torch.int32, device=DEV)
+    binding.ragged_attn_backward(*lot[:3], lot[4], lot[3], one_lse.repeat(many, 1), *grads, ends, n, 0.125)
+    for a, b in zip(few, grads):
+        assert torch.equal(a.repeat(many, 1, 1), b.cpu())
